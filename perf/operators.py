@@ -1,0 +1,598 @@
+"""Attention of drafted trees over a paged cache, and the calls that keep that cache, as measurable cases.
+
+Four kinds of case, by what a speculative-decoding step calls:
+
+* ``attention``: one layer's attention of every sequence's drafted tokens over its pages (`tree_attention`);
+* ``append``: one layer's new keys and values written into the pages (`cache_append`);
+* ``turn``: what a step does to the cache around the model: pages for the drafted tokens, the ancestor masks of their
+  trees, their keys and values in all layers, the accepted path moved together, surplus pages given back
+  (`cache_set_lens`, `cache_reserve`, `tree_mask`, `cache_append`, `cache_compact`, `cache_set_lens`);
+* ``fork``: finished branches freed and new ones forked from their parents (`cache_set_lens`, `cache_fork`).
+
+`run` makes these calls where `own` is true and computes the same in elementary torch operations where it is not.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def listed():
+    return [
+        # one new token of one request at the start of an answer: launches and host work are all there is
+        dict(name="attn_one_token", op="attention", dtype="bf16", n=1, T=1, ragged=False, lo=500, hi=500, hq=32, hkv=8, D=128, P=16, tree=False),
+        # a small batch of short contexts with odd counts throughout: five query heads to a key head, a head of 80, 13 drafted tokens at most
+        dict(name="attn_odd_tree", op="attention", dtype="f16", n=7, T=13, ragged=True, lo=3, hi=1501, hq=40, hkv=8, D=80, P=32, tree=True),
+        # the large serving batch of the head's benchmark: 64 requests of 8 tree positions, contexts of all lengths
+        dict(name="attn_batch_tree", op="attention", dtype="bf16", n=64, T=8, ragged=False, lo=130, hi=4100, hq=32, hkv=8, D=128, P=16, tree=True),
+        # one request with a long document and a wide tree: few rows, a long axis
+        dict(name="attn_long_context", op="attention", dtype="bf16", n=1, T=48, ragged=False, lo=131000, hi=131000, hq=32, hkv=8, D=128, P=64, tree=True),
+        # verification of wide trees by a model with many query heads to a key head: 512 rows for each key head, bound by products
+        dict(name="attn_wide_trees", op="attention", dtype="bf16", n=16, T=64, ragged=False, lo=2000, hi=10000, hq=64, hkv=8, D=64, P=32, tree=True),
+        # single tokens of many long requests: the whole of a cache of 8 GB read once
+        dict(name="attn_decode_large", op="attention", dtype="f16", n=128, T=1, ragged=False, lo=15000, hi=17400, hq=32, hkv=8, D=128, P=64, tree=False),
+        # drafted tokens of a batch, one layer
+        dict(name="append_batch", op="append", dtype="bf16", n=64, T=8, ragged=True, lo=100, hi=4000, hkv=8, D=128, P=16),
+        # prompts of a few requests, one layer
+        dict(name="append_prompts", op="append", dtype="f16", n=4, T=8192, ragged=True, lo=0, hi=500, hkv=8, D=128, P=64),
+        # a step of one request: a drafter of one layer
+        dict(name="turn_one", op="turn", dtype="bf16", n=1, T=8, ragged=False, lo=700, hi=700, layers=1, hkv=8, D=128, P=16),
+        # a step of the large batch: a model of 32 layers
+        dict(name="turn_batch", op="turn", dtype="bf16", n=64, T=8, ragged=True, lo=90, hi=300, layers=32, hkv=8, D=128, P=16),
+        # one request answered four times
+        dict(name="fork_one", op="fork", dtype="bf16", n=1, kids=4, lo=1000, hi=1000, layers=1, hkv=8, D=128, P=16),
+        # many requests with several answers each, all layers, long pages
+        dict(name="fork_batch", op="fork", dtype="f16", n=24, kids=4, lo=200, hi=2100, layers=32, hkv=4, D=128, P=64),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    """An integer in [lo, hi], uniform over its logarithm."""
+    return max(lo, min(hi, int(round(lo * (hi / lo) ** rng.random()))))
+
+
+def draw(rng):
+    op = rng.choice(["attention", "attention", "attention", "attention", "append", "turn", "fork"])
+    c = dict(op=op, dtype=rng.choice(["bf16", "f16"]), P=rng.choice([16, 32, 64, 128]), D=rng.choice([64, 128, 128, 128, 80, 96, 256]))
+    c["hkv"] = rng.choice([1, 2, 3, 4, 8, 8])
+    if op == "attention":
+        c["hq"] = c["hkv"] * rng.choice([1, 2, 4, 4, 5, 8, 7])
+        c["tree"] = rng.random() < 0.7
+        c["T"] = rng.choice([1, rng.randint(2, 16), _log_int(rng, 2, 130)])
+        c["n"] = _log_int(rng, 1, 128)
+        c["ragged"] = rng.random() < 0.5
+        c["hi"] = _log_int(rng, 20, 131000)
+        # keep below the listed cases: cached values read, products of the rows
+        while c["n"] > 1 and c["n"] * c["hi"] * c["hkv"] * c["D"] > 1 << 31:
+            c["n"] = (c["n"] + 1) // 2
+        while c["n"] * c["hi"] * c["T"] * c["hq"] * c["D"] > 16 * 6000 * 64 * 64 * 64:
+            c["hi"] = max(1, c["hi"] // 2)
+            c["n"] = (c["n"] + 1) // 2
+        c["lo"] = rng.randint(0, c["hi"])
+    elif op == "append":
+        c["n"] = _log_int(rng, 1, 128)
+        c["T"] = _log_int(rng, 1, max(1, 16000 // c["n"]))
+        c["ragged"] = rng.random() < 0.5
+        c["hi"] = _log_int(rng, 1, 4000)
+        c["lo"] = rng.randint(0, c["hi"])
+    elif op == "turn":
+        c["n"] = _log_int(rng, 1, 64)
+        c["T"] = _log_int(rng, 1, 64)
+        c["ragged"] = rng.random() < 0.5
+        c["layers"] = _log_int(rng, 1, 32)
+        while c["n"] * c["T"] * c["layers"] * c["hkv"] * c["D"] > 64 * 8 * 32 * 1024:
+            c["T"] = (c["T"] + 1) // 2
+            c["layers"] = (c["layers"] + 1) // 2
+        c["hi"] = _log_int(rng, 1, 300)
+        c["lo"] = rng.randint(0, c["hi"])
+    else:
+        c["n"] = _log_int(rng, 1, 24)
+        c["kids"] = rng.randint(1, 5)
+        c["layers"] = _log_int(rng, 1, 32)
+        while c["n"] * c["kids"] * c["layers"] * c["hkv"] * c["D"] * c["P"] > 24 * 4 * 32 * 512 * 64:
+            c["n"] = (c["n"] + 1) // 2
+            c["layers"] = (c["layers"] + 1) // 2
+        c["hi"] = _log_int(rng, 1, 2100)
+        c["lo"] = rng.randint(1, c["hi"])
+    return c
+
+
+def _counts(c):
+    """New tokens of every sequence: T, or where ragged anything from 1 to T."""
+    return [1 + (i * 7919) % c["T"] if c["ragged"] else c["T"] for i in range(c["n"])]
+
+
+def _contexts(c):
+    """Committed tokens of every sequence: spread evenly from lo to hi, in a fixed odd order."""
+    n = c["n"]
+    even = [c["lo"] + (c["hi"] - c["lo"]) * i // max(1, n - 1) for i in range(n)]
+    step = next(s for s in (7, 11, 13, 17, 1) if math.gcd(s, n) == 1)
+    return [even[i * step % n] for i in range(n)]
+
+
+def _accepted(c):
+    """Accepted tokens of every sequence in a turn: one to six of its drafted ones."""
+    return [min(t, 1 + (5 * i + 2) % 6) for i, t in enumerate(_counts(c))]
+
+
+def _pages(tokens, P):
+    return -(-tokens // P)
+
+
+def work(case):
+    c, esize = case, 2
+    row = c["hkv"] * c["D"] * esize * 2                    # a token's keys and values in one layer
+    if c["op"] == "attention":
+        counts, ctx = _counts(c), _contexts(c)
+        q = sum(counts) * c["hq"] * c["D"] * esize
+        table = sum(4 * _pages(x + t, c["P"]) for x, t in zip(ctx, counts))
+        return {"bytes": sum(x + t for x, t in zip(ctx, counts)) * row + 2 * q + sum(counts) * (4 * c["hq"] + (8 * -(-c["T"] // 64) if c["tree"] else 0)) + table,
+                "flops": sum(4 * t * c["hq"] * c["D"] * (x + 1) for x, t in zip(ctx, counts))}
+    if c["op"] == "append":
+        return {"bytes": 2 * sum(_counts(c)) * row, "flops": 0}
+    if c["op"] == "turn":
+        # every drafted row in and out; accepted ones but the first, which is in its place, are read and written again
+        return {"bytes": 2 * c["layers"] * row * sum(t + a - 1 for t, a in zip(_counts(c), _accepted(c))), "flops": 0}
+    # the rows of a parent's last page are read once and written for each child; the shared pages' entries and counts move
+    tails = sum(x % c["P"] for x in _contexts(c))
+    shared = sum(x // c["P"] for x in _contexts(c))
+    return {"bytes": c["layers"] * row * tails * (1 + c["kids"]) + 8 * shared * (1 + c["kids"]) + 16 * c["n"] * c["kids"], "flops": 0}
+
+
+# ---------------------------------------------------------------------------------------------------------- inputs
+
+
+def _ints(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def _cache(c, g, lens, tokens, spare_slots=0, spare_pages=0):
+    """A cache whose slot i holds the pages of tokens[i] tokens, scattered over the pool, all values drawn: pages keep what was in them."""
+    layers, P = c.get("layers", 1), c["P"]
+    need = [_pages(t, P) for t in tokens]
+    pages = max(1, sum(need) + spare_pages)
+    width = max(1, max(need) + 2, _pages(max(tokens) + c.get("T", 0), P) + 1)
+    shape = (layers, pages, c["hkv"], P, c["D"])
+    k = torch.randn(shape, generator=g, device="cuda", dtype=DTYPES[c["dtype"]])
+    v = torch.randn(shape, generator=g, device="cuda", dtype=DTYPES[c["dtype"]])
+    order = torch.randperm(pages, generator=g, device="cuda").to(torch.int32).cpu()
+    slots = c["n"] + spare_slots
+    table = torch.zeros((slots, width), dtype=torch.int32)
+    refs = torch.zeros(pages, dtype=torch.int32)
+    at = 0
+    for i, m in enumerate(need):
+        table[i, :m] = order[at:at + m]
+        refs[order[at:at + m].long()] = 1
+        at += m
+    held = torch.tensor(need + [0] * spare_slots, dtype=torch.int32)
+    lens = torch.tensor(list(lens) + [0] * spare_slots, dtype=torch.int32)
+    return dict(k=k, v=v, table=table.cuda(), held=held.cuda(), lens=lens.cuda(), refs=refs.cuda())
+
+
+def _trees(counts, accepted, g):
+    """Parents of every drafted token (its index in the sequence's tree, -1: the root) and a path from the root in each tree."""
+    width = max(accepted)
+    total = sum(counts)
+    pick = torch.rand(total, generator=g, device="cuda").tolist()
+    parents, paths, at = [], [], 0
+    for t, a in zip(counts, accepted):
+        rest = sorted(range(1, t), key=lambda j: pick[at + j])[:a - 1]
+        path = [0] + sorted(rest)
+        up = [-1] + [int(pick[at + j] * 7919) % j for j in range(1, t)]
+        for x, y in zip(path, path[1:]):
+            up[y] = x
+        parents += up
+        paths.append(path + [0] * (width - a))
+        at += t
+    return parents, paths
+
+
+def prepare(case, seed):
+    c = case
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = DTYPES[c["dtype"]]
+    ctx = _contexts(c)
+    s = dict(case=c, op=c["op"])
+    if c["op"] == "fork":
+        # the children still hold branches of their own that are over: some pages each, of no parent
+        kids = c["n"] * c["kids"]
+        old = [1 + (13 * i) % (2 * c["P"]) for i in range(kids)]
+        both = dict(c, n=c["n"] + kids)
+        s.update(_cache(both, g, ctx + old, ctx + old, spare_pages=kids + 3))
+        # rows of the table wide enough for the longest parent are there already: a child takes its parent's place
+        s["parents"] = _ints([i for i in range(c["n"]) for _ in range(c["kids"])])
+        s["children"] = _ints([c["n"] + i for i in range(kids)])
+        s["report"] = _ints([0])
+    else:
+        counts = _counts(c)
+        total = sum(counts)
+        cu = [0]
+        for t in counts:
+            cu.append(cu[-1] + t)
+        s["cu"] = _ints(cu)
+        s["total"], s["most"] = total, max(counts)
+        s["slots"] = torch.randperm(c["n"], generator=g, device="cuda").to(torch.int32)
+        back = s["slots"].cpu().tolist()                       # sequence i of the call lives in slot back[i]
+        in_slot = lambda xs: [xs[back.index(j)] for j in range(c["n"])]  # noqa: E731
+        at, drafted = in_slot(ctx), in_slot(counts)
+        if c["op"] == "turn":
+            # the slots stand as the step before left them: settled, with what that step had drafted still held by some
+            s.update(_cache(c, g, at, [x + (i % 3) * c["P"] for i, x in enumerate(at)], spare_pages=sum(_pages(t, c["P"]) + 1 for t in counts) + 5))
+            s["base"] = _ints(ctx)
+            s["new_lens"], s["report"] = _ints([0] * c["n"]), _ints([0])
+            accepted = _accepted(c)
+            parents, paths = _trees(counts, accepted, g)
+            s["parents"], s["path"], s["accepted"] = _ints(parents), _ints(paths), _ints(accepted)
+            s["words"] = -(-max(counts) // 64)
+            s["mask"] = torch.zeros((total, s["words"]), dtype=torch.int64, device="cuda")
+            new = (c["layers"], total, c["hkv"], c["D"])
+        else:
+            s.update(_cache(c, g, at, [x + t for x, t in zip(at, drafted)]))
+            new = (total, c["hkv"], c["D"])
+        if c["op"] == "attention":
+            # keys of unequal channels, as projections give them: scores spread over a few units
+            s["k"] *= (0.5 + torch.rand(c["D"], generator=g, device="cuda")).to(dt)
+            s["q"] = torch.randn((total, c["hq"], c["D"]), generator=g, device="cuda").mul_(1.5).to(dt)
+            s["scale"] = c["D"] ** -0.5
+            s["out"] = torch.zeros_like(s["q"])
+            s["lse"] = torch.zeros((total, c["hq"]), dtype=torch.float32, device="cuda")
+            s["mask"] = None
+            if c["tree"]:
+                parents, _ = _trees(counts, [1] * c["n"], g)
+                words = -(-max(counts) // 64)
+                rows, first = [], 0
+                for t in counts:
+                    bits = []
+                    for j in range(t):
+                        p = parents[first + j]
+                        bits.append((bits[p] if p >= 0 else 0) | 1 << j)
+                    rows += bits
+                    first += t
+                full = 1 << 64
+                sign = lambda x: x - full if x >> 63 else x  # noqa: E731
+                s["mask"] = torch.tensor([[sign(b >> 64 * w & full - 1) for w in range(words)] for b in rows], dtype=torch.int64, device="cuda")
+        else:
+            s["k_new"] = torch.randn(new, generator=g, device="cuda", dtype=dt)
+            s["v_new"] = torch.randn(new, generator=g, device="cuda", dtype=dt)
+    if own:
+        # what a program keeps beside the tensors: the cache's description, and scratch for the calls
+        from paper_2605_10453_amd import binding
+        s["cache"] = binding.PagedCache(s["k"], s["v"], s["table"], s["held"], s["lens"], s["refs"])
+        if c["op"] == "attention":
+            s["workspace"] = binding.tree_attention_workspace(s["cache"], c["n"], s["total"], c["hq"])
+    return s
+
+
+# ----------------------------------------------------------------------------------------------------------- calls
+
+
+def run(state):
+    return (_OWN if own else _PLAIN)[state["op"]](state)
+
+
+def _own_attention(s):
+    from paper_2605_10453_amd import binding
+    out, lse = binding.tree_attention(s["cache"], 0, s["q"], s["slots"], s["cu"], mask=s["mask"], scale=s["scale"], out=s["out"], lse=s["lse"],
+                                      workspace=s["workspace"])
+    return {"out": out, "lse": lse}
+
+
+def _own_append(s):
+    from paper_2605_10453_amd import binding
+    binding.cache_append(s["cache"], 0, s["k_new"], s["v_new"], s["slots"], s["cu"])
+    return {"k": s["k"], "v": s["v"]}
+
+
+def _own_turn(s):
+    from paper_2605_10453_amd import binding
+    c = s["cache"]
+    binding.cache_set_lens(c, s["slots"], s["base"])
+    binding.cache_reserve(c, s["slots"], s["cu"], report=s["report"])
+    mask = binding.tree_mask(s["parents"], s["cu"], s["words"], out=s["mask"])
+    binding.cache_append(c, 0, s["k_new"], s["v_new"], s["slots"], s["cu"])
+    binding.cache_compact(c, s["slots"], s["path"], s["accepted"], new_lens=s["new_lens"])
+    binding.cache_set_lens(c, s["slots"], s["new_lens"])
+    return {"mask": mask, "k": s["k"], "v": s["v"], "table": s["table"], "held": s["held"], "lens": s["lens"], "refs": s["refs"], "report": s["report"]}
+
+
+def _own_fork(s):
+    from paper_2605_10453_amd import binding
+    binding.cache_set_lens(s["cache"], s["children"], None)
+    binding.cache_fork(s["cache"], s["parents"], s["children"], report=s["report"])
+    return {"k": s["k"], "v": s["v"], "table": s["table"], "held": s["held"], "lens": s["lens"], "refs": s["refs"], "report": s["report"]}
+
+
+def _sequence_of(cu, total):
+    """Of every token the sequence it belongs to, and its index there."""
+    token = torch.arange(total, device=cu.device)
+    seq = torch.searchsorted(cu[1:].long(), token, right=True)
+    return seq, token - cu.long()[seq]
+
+
+def _plain_attention(s):
+    k, v, q, P = s["k"][0], s["v"][0], s["q"], s["k"].shape[3]
+    total, hq, D = q.shape
+    hkv, n, most = k.shape[1], s["slots"].numel(), s["most"]
+    G = hq // hkv
+    lens = s["lens"].long()[s["slots"].long()]
+    counts = (s["cu"][1:] - s["cu"][:-1]).long()
+    width = _pages(max(x + t for x, t in zip(_contexts(s["case"]), _counts(s["case"]))), P)
+    pages = s["table"][s["slots"].long(), :width].long()
+    def gather(x):
+        return x[pages].permute(0, 2, 1, 3, 4).reshape(n, hkv, width * P, D).float()
+    seq, t = _sequence_of(s["cu"], total)
+    padded = torch.zeros((n, most, hq, D), device=q.device)
+    padded[seq, t] = q.float()
+    rows = padded.view(n, most, hkv, G, D).permute(0, 2, 1, 3, 4).reshape(n, hkv, most * G, D)
+    scores = torch.matmul(rows, gather(k).transpose(2, 3)).view(n, hkv, most, G, width * P).mul_(s["scale"])
+    place = torch.arange(width * P, device=q.device)
+    draft = place[None] - lens[:, None]                                             # [n, places]: which drafted token lies there
+    index = torch.arange(most, device=q.device)
+    if s["mask"] is None:
+        seen = draft[:, None, :] <= index[None, :, None]
+    else:
+        words = torch.zeros((n, most, s["mask"].shape[1]), dtype=torch.int64, device=q.device)
+        words[seq, t] = s["mask"]
+        d = draft.clamp(0, 64 * words.shape[2] - 1)
+        bit = torch.gather(words, 2, (d // 64)[:, None, :].expand(n, most, -1)) >> (d % 64)[:, None, :] & 1
+        seen = (draft < 0)[:, None, :] | (bit == 1)
+    seen = seen & (draft < counts[:, None])[:, None, :]
+    scores.masked_fill_(~seen[:, None, :, None, :], -math.inf)
+    top = scores.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    p = scores.sub_(top).exp_()
+    total_p = p.sum(-1, keepdim=True)
+    o = torch.matmul(p.view(n, hkv, most * G, width * P), gather(v)).view(n, hkv, most, G, D)
+    o = torch.where(total_p > 0, o / total_p, torch.zeros_like(o))
+    lse = (total_p.log() + top).squeeze(-1)
+    out = o.permute(0, 2, 1, 3, 4).reshape(n, most, hq, D)[seq, t]
+    s["out"].copy_(out)
+    s["lse"].copy_(lse.permute(0, 2, 1, 3).reshape(n, most, hq)[seq, t])
+    return {"out": s["out"], "lse": s["lse"]}
+
+
+def _plain_write(s, k_new, v_new):
+    """New rows [layers, tokens, heads, D] to the places behind the committed tokens."""
+    P = s["k"].shape[3]
+    seq, t = _sequence_of(s["cu"], k_new.shape[1])
+    slot = s["slots"].long()[seq]
+    place = s["lens"].long()[slot] + t
+    page = s["table"].long()[slot, place // P]
+    s["k"][:, page, :, place % P] = k_new.transpose(0, 1)
+    s["v"][:, page, :, place % P] = v_new.transpose(0, 1)
+
+
+def _plain_append(s):
+    _plain_write(s, s["k_new"][None], s["v_new"][None])
+    return {"k": s["k"], "v": s["v"]}
+
+
+def _plain_set_lens(s, slots, lens):
+    P = s["k"].shape[3]
+    slots = slots.long()
+    lens = torch.zeros_like(s["lens"][slots]) if lens is None else lens
+    keep = torch.minimum((lens + P - 1) // P, s["held"][slots])
+    col = torch.arange(s["table"].shape[1], device=keep.device)
+    over = (col >= keep[:, None]) & (col < s["held"][slots][:, None])
+    s["refs"].index_add_(0, torch.where(over, s["table"][slots], 0).reshape(-1), -over.reshape(-1).to(torch.int32))
+    s["held"][slots] = keep
+    s["lens"][slots] = lens
+
+
+def _plain_take(s, wanted):
+    """The first `wanted` (a tensor) free pages, lowest first, in an array as long as the pool; they are marked as held once."""
+    free = s["refs"] == 0
+    rank = free.long().cumsum(0) - 1
+    pages = torch.zeros_like(s["refs"])
+    spill = torch.zeros(s["refs"].numel() + 1, dtype=torch.int32, device=pages.device)
+    spill[torch.where(free, rank, s["refs"].numel())] = torch.arange(s["refs"].numel(), dtype=torch.int32, device=pages.device)
+    s["refs"].add_((free & (rank < wanted)).to(torch.int32))
+    return spill[:-1]
+
+
+def _plain_reserve(s):
+    P, slots = s["k"].shape[3], s["slots"].long()
+    counts = s["cu"][1:] - s["cu"][:-1]
+    held = s["held"][slots]
+    need = torch.clamp((s["lens"][slots] + counts + P - 1) // P - held, min=0)
+    before = need.cumsum(0) - need
+    pages = _plain_take(s, need.sum())
+    col = torch.arange(s["table"].shape[1], device=need.device)
+    new = (col >= held[:, None]) & (col < (held + need)[:, None])
+    rank = torch.where(new, before[:, None] + col - held[:, None], 0)
+    s["table"][slots] = torch.where(new, pages[rank], s["table"][slots])
+    s["held"][slots] = held + need.to(torch.int32)
+    s["report"].zero_()
+
+
+def _plain_mask(s):
+    """Bits of every token's ancestors and its own: the set of parents' parents doubles its reach until the longest chain is covered."""
+    seq, t = _sequence_of(s["cu"], s["total"])
+    n, most, words = s["slots"].numel(), s["most"], s["words"]
+    up = torch.zeros((n, most, most), device=t.device)
+    parent = s["parents"].long()
+    up[seq, t, t] = 1
+    up[seq, t, torch.where(parent < 0, t, parent)] = 1
+    for _ in range(max(1, math.ceil(math.log2(max(2, most))))):
+        up = (torch.matmul(up, up) > 0).float()
+    bits = torch.zeros((s["total"], words * 64), dtype=torch.int64, device=t.device)
+    bits[:, :most] = up[seq, t].long()
+    s["mask"].copy_((bits.view(-1, words, 64) << torch.arange(64, device=t.device)).sum(-1))
+    return s["mask"]
+
+
+def _plain_compact(s):
+    P, slots = s["k"].shape[3], s["slots"].long()
+    lens, a = s["lens"].long()[slots], s["accepted"].long()
+    j = torch.arange(s["path"].shape[1], device=lens.device)
+    kept = j[None] < a[:, None]
+    # rows that are not kept are written onto themselves
+    to = lens[:, None] + torch.where(kept, j[None], 0)
+    source = lens[:, None] + torch.where(kept, s["path"].long(), s["path"].long()[:, :1])
+    table = s["table"].long()[slots]
+    to_page, from_page = torch.gather(table, 1, to // P).view(-1), torch.gather(table, 1, source // P).view(-1)
+    to, source = to.view(-1) % P, source.view(-1) % P
+    s["k"][:, to_page, :, to] = s["k"][:, from_page, :, source]
+    s["v"][:, to_page, :, to] = s["v"][:, from_page, :, source]
+    s["new_lens"].copy_(lens + a)
+
+
+def _plain_turn(s):
+    _plain_set_lens(s, s["slots"], s["base"])
+    _plain_reserve(s)
+    mask = _plain_mask(s)
+    _plain_write(s, s["k_new"], s["v_new"])
+    _plain_compact(s)
+    _plain_set_lens(s, s["slots"], s["new_lens"])
+    return {"mask": mask, "k": s["k"], "v": s["v"], "table": s["table"], "held": s["held"], "lens": s["lens"], "refs": s["refs"], "report": s["report"]}
+
+
+def _plain_fork(s):
+    P = s["k"].shape[3]
+    _plain_set_lens(s, s["children"], None)
+    parents, children = s["parents"].long(), s["children"].long()
+    lens = s["lens"][parents]
+    full, own_page = lens // P, (lens % P > 0).to(torch.int32)
+    rank = own_page.cumsum(0) - own_page
+    pages = _plain_take(s, own_page.sum())
+    col = torch.arange(s["table"].shape[1], device=lens.device)
+    shared = col < full[:, None]
+    source = s["table"][parents]
+    s["refs"].index_add_(0, torch.where(shared, source, 0).reshape(-1), shared.reshape(-1).to(torch.int32))
+    mine = (col == full[:, None]) & (own_page == 1)[:, None]
+    s["table"][children] = torch.where(shared, source, torch.where(mine, pages[rank][:, None], s["table"][children]))
+    s["held"][children] = full + own_page
+    s["lens"][children] = lens
+    # the tail's rows; a child without a tail copies its parent's first page onto that page
+    at = torch.where(own_page == 1, full, 0).long()[:, None]
+    old = torch.gather(source, 1, at).view(-1).long()
+    new = torch.where(own_page == 1, torch.gather(s["table"][children], 1, at).view(-1), old.int()).long()
+    row = torch.arange(P, device=lens.device)
+    keep = (row >= (lens % P)[:, None]) & (own_page == 1)[:, None]
+    for x in (s["k"], s["v"]):
+        x[:, new] = torch.where(keep[None, :, None, :, None], x[:, new], x[:, old])
+    s["report"].zero_()
+    return {"k": s["k"], "v": s["v"], "table": s["table"], "held": s["held"], "lens": s["lens"], "refs": s["refs"], "report": s["report"]}
+
+
+_OWN = {"attention": _own_attention, "append": _own_append, "turn": _own_turn, "fork": _own_fork}
+_PLAIN = {"attention": _plain_attention, "append": _plain_append, "turn": _plain_turn, "fork": _plain_fork}
+
+
+# -------------------------------------------------------------------------------------------- the definition, in 64 bits
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"attention": _exact_attention, "append": _exact_append, "turn": _exact_turn, "fork": _exact_fork}[case["op"]](s)
+
+
+def _exact_attention(s):
+    out, lse = torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda"), torch.zeros(s["lse"].shape, dtype=torch.float64, device="cuda")
+    cu, slots, lens, table = s["cu"].tolist(), s["slots"].tolist(), s["lens"].tolist(), s["table"].cpu()
+    P, hkv = s["k"].shape[3], s["k"].shape[2]
+    G = s["q"].shape[1] // hkv
+    mask = None if s["mask"] is None else s["mask"].cpu().tolist()
+    for i, slot in enumerate(slots):
+        L, T = lens[slot], cu[i + 1] - cu[i]
+        place = torch.arange(L + T)
+        page, row = table[slot, place // P].long().cuda(), (place % P).cuda()
+        tree = torch.tensor([[(a <= b) if mask is None else bool(mask[cu[i] + b][a // 64] >> a % 64 & 1) for a in range(T)] for b in range(T)])
+        seen = torch.cat([torch.ones((T, L), dtype=torch.bool), tree], 1).cuda()
+        for h in range(hkv):
+            K, V = s["k"][0, page, h, row].double(), s["v"][0, page, h, row].double()
+            x = torch.einsum("tgd,pd->tgp", s["q"][cu[i]:cu[i + 1], h * G:(h + 1) * G].double(), K) * s["scale"]
+            x = x.masked_fill(~seen[:, None], -math.inf)
+            at = torch.logsumexp(x, -1)
+            lse[cu[i]:cu[i + 1], h * G:(h + 1) * G] = at
+            out[cu[i]:cu[i + 1], h * G:(h + 1) * G] = torch.einsum("tgp,pd->tgd", torch.exp(x - at[..., None]), V)
+    return {"out": out, "lse": lse}
+
+
+def _host(s):
+    """The books of a cache as lists: they are kept token by token and page by page below."""
+    return s["table"].tolist(), s["held"].tolist(), s["lens"].tolist(), s["refs"].tolist()
+
+
+def _exact_append(s):
+    table, _, lens, _ = _host(s)
+    cu, P = s["cu"].tolist(), s["k"].shape[3]
+    for i, slot in enumerate(s["slots"].tolist()):
+        t = 0
+        while t < cu[i + 1] - cu[i]:                          # runs within a page
+            place = lens[slot] + t
+            m = min(P - place % P, cu[i + 1] - cu[i] - t)
+            for x, new in ((s["k"], s["k_new"]), (s["v"], s["v_new"])):
+                x[0, table[slot][place // P], :, place % P:place % P + m] = new[cu[i] + t:cu[i] + t + m].transpose(0, 1)
+            t += m
+    return {"k": s["k"], "v": s["v"]}
+
+
+def _settle(slot, length, P, table, held, lens, refs):
+    while held[slot] > -(-length // P):
+        held[slot] -= 1
+        refs[table[slot][held[slot]]] -= 1
+    lens[slot] = length
+
+
+def _exact_turn(s):
+    table, held, lens, refs = _host(s)
+    cu, P, slots = s["cu"].tolist(), s["k"].shape[3], s["slots"].tolist()
+    base, path, accepted, parents = s["base"].tolist(), s["path"].tolist(), s["accepted"].tolist(), s["parents"].tolist()
+    for slot, x in zip(slots, base):
+        _settle(slot, x, P, table, held, lens, refs)
+    for i, slot in enumerate(slots):
+        while held[slot] * P < lens[slot] + cu[i + 1] - cu[i]:
+            page = refs.index(0)
+            refs[page] = 1
+            table[slot][held[slot]] = page
+            held[slot] += 1
+    rows = []
+    for i, slot in enumerate(slots):
+        bits = []
+        for t in range(cu[i + 1] - cu[i]):
+            p, b = parents[cu[i] + t], 1 << t
+            while p >= 0:
+                b |= 1 << p
+                p = parents[cu[i] + p]
+            bits.append(b)
+        rows += bits
+        for t in range(cu[i + 1] - cu[i]):                    # every drafted row, then the accepted ones again, where they end up
+            place = lens[slot] + t
+            for x, new in ((s["k"], s["k_new"]), (s["v"], s["v_new"])):
+                x[:, table[slot][place // P], :, place % P] = new[:, cu[i] + t]
+        for j in range(accepted[i]):
+            place = lens[slot] + j
+            for x, new in ((s["k"], s["k_new"]), (s["v"], s["v_new"])):
+                x[:, table[slot][place // P], :, place % P] = new[:, cu[i] + path[i][j]]
+        _settle(slot, lens[slot] + accepted[i], P, table, held, lens, refs)
+    full = 1 << 64
+    sign = [[(b >> 64 * w & full - 1) - (full if b >> 64 * w + 63 & 1 else 0) for w in range(s["words"])] for b in rows]
+    return {"mask": torch.tensor(sign, dtype=torch.int64), "k": s["k"], "v": s["v"], "table": _ints(table), "held": _ints(held), "lens": _ints(lens),
+            "refs": _ints(refs), "report": _ints([0])}
+
+
+def _exact_fork(s):
+    table, held, lens, refs = _host(s)
+    P = s["k"].shape[3]
+    pairs = list(zip(s["parents"].tolist(), s["children"].tolist()))
+    for _, child in pairs:
+        _settle(child, 0, P, table, held, lens, refs)
+    for parent, child in pairs:
+        full, rest = divmod(lens[parent], P)
+        for j in range(full):
+            table[child][j] = table[parent][j]
+            refs[table[parent][j]] += 1
+        if rest:
+            page = refs.index(0)
+            refs[page] = 1
+            table[child][full] = page
+            for x in (s["k"], s["v"]):
+                x[:, page, :, :rest] = x[:, table[parent][full], :, :rest]
+        held[child], lens[child] = full + (rest > 0), lens[parent]
+    return {"k": s["k"], "v": s["v"], "table": _ints(table), "held": _ints(held), "lens": _ints(lens), "refs": _ints(refs), "report": _ints([0])}
