@@ -295,7 +295,7 @@ def _own_turn(s):
     binding.cache_reserve(c, s["slots"], s["cu"], report=s["report"])
     mask = binding.tree_mask(s["parents"], s["cu"], s["words"], out=s["mask"])
     binding.cache_append(c, 0, s["k_new"], s["v_new"], s["slots"], s["cu"])
-    binding.cache_compact(c, s["slots"], s["path"], s["accepted"], new_lens=s["new_lens"])
+    binding.cache_compact(c, s["slots"], s["cu"], s["path"], s["accepted"], new_lens=s["new_lens"])
     binding.cache_set_lens(c, s["slots"], s["new_lens"])
     return {"mask": mask, "k": s["k"], "v": s["v"], "table": s["table"], "held": s["held"], "lens": s["lens"], "refs": s["refs"], "report": s["report"]}
 
