@@ -66,7 +66,8 @@ typedef struct slimspec_shape {
 
 typedef enum slimspec_dtype {
     SLIMSPEC_BF16 = 0,
-    SLIMSPEC_F32 = 1
+    SLIMSPEC_F32 = 1,
+    SLIMSPEC_F16 = 2        /* caches only: the heads take BF16 and, for W, F32 */
 } slimspec_dtype;
 
 typedef enum slimspec_status {
@@ -245,6 +246,116 @@ int routed_head_topk_prepared(const void *h, const void *A, const void *B, const
                               int32_t *out_ids, float *out_logprobs,
                               void *workspace, size_t workspace_bytes,
                               void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Drafted trees over a paged key/value cache.  What follows the head in a speculative step: the
+ * tokens that it drafted attend to their sequence's cache and to their own ancestors, the accepted
+ * path stays in the cache, and sequences share, copy and give back pages.
+ *
+ * The cache.  Keys and values lie in a pool of pages of page_size places each, the same layout for
+ * both: element (layer, page, head, place, c) of k and v is at
+ *     layer * layer_stride + page * page_stride + head * head_stride + place * place_stride + c
+ * (strides in elements; so pages may keep heads or places outermost).  The books, all int32:
+ *     table [slots, slot_pages]   page of each of a slot's stretches of page_size tokens
+ *     held  [slots]               how many pages the slot holds: table entries at and past it mean nothing
+ *     lens  [slots]               tokens committed; drafted tokens lie in the places behind them
+ *     refs  [pages]               slots that hold the page; 0: the page is free
+ * An empty cache has held, lens and refs zero.  A page that more than one slot holds is full and
+ * never written again: a fork gets its own copy of a page that is not full.
+ *
+ * A batch names the sequences of a call: sequence i lives in slot slots[i] and brings the new
+ * (drafted) tokens first[i] .. first[i + 1] - 1 of the call's `tokens` (first: n + 1 entries), which
+ * lie at places lens[slot] on.  A sequence may bring none.  The slots of a call are distinct.
+ *
+ * k, v, the books and the arrays of a batch are DEVICE memory of the caller; k, v, refs and all
+ * rows of keys, values, queries and outputs are 16-byte aligned; strides are multiples of 8.
+ * slimspec_cache and slimspec_batch themselves are read on the host during the call only.
+ * Ownership, asynchrony and errors as above; what stands in device memory cannot be checked before
+ * the call returns, so the kernels bound it themselves: a sequence whose slot, token range or
+ * length is out of range is left out, a page number out of range counts as no page (nothing is
+ * read or written there; attention does not see its tokens).
+ *
+ * Supported: BF16 and F16; head_dim a multiple of 8 up to SLIMSPEC_CACHE_MAX_HEAD_DIM; page_size a
+ * power of two, 16 to 1024; up to SLIMSPEC_CACHE_MAX_SEQUENCES sequences a call; slot_pages *
+ * page_size < 2^31; place_stride <= 2^20.  Element offsets are 64 bits throughout. */
+#define SLIMSPEC_CACHE_MAX_HEAD_DIM 256
+#define SLIMSPEC_CACHE_MAX_SEQUENCES 4096
+#define SLIMSPEC_TREE_MAX_WORDS 64
+
+typedef struct slimspec_cache {
+    void *k, *v;
+    int64_t layer_stride, page_stride, head_stride, place_stride;
+    int32_t *table, *held, *lens, *refs;
+    int32_t layers, pages, heads, page_size, head_dim;
+    int32_t slots, slot_pages;
+    slimspec_dtype dtype;
+} slimspec_cache;
+
+typedef struct slimspec_batch {
+    const int32_t *slots;       /* [n]     */
+    const int32_t *first;       /* [n + 1] */
+    int32_t n;                  /* sequences, >= 0 */
+    int32_t tokens;             /* rows of the call's token arrays, >= 0 */
+} slimspec_batch;
+
+/* Attention of the new tokens, one layer.  q [tokens, q_heads, head_dim] in the cache's type
+ * (element (t, h, c) at t * q_token_stride + h * q_head_stride + c), q_heads a multiple of the
+ * cache's heads: query head h reads key head h / (q_heads / heads).  Token t of a sequence with L
+ * committed tokens sees S(t) = the committed places 0 .. L - 1 and, of the sequence's new tokens j,
+ *     mask given: those with bit j % 64 of word j / 64 of mask[t] set (mask [tokens, mask_words]
+ *                 64-bit words, row-major; its own bit too only if set; none beyond the words);
+ *     mask null:  j <= t, the chain of plain decoding (one new token: the single-token form).
+ * The keys and values of the new tokens are read from the cache (slimspec_cache_append).
+ *     s_p = scale * sum_c q_c k_pc,   lse = ln sum_{p in S} exp(s_p),   out = sum_{p in S} exp(s_p - lse) v_p
+ * out [tokens, q_heads, head_dim] with strides of its own; lse [tokens, q_heads] float or null.  A
+ * token that sees nothing has out = 0 and lse = -infinity.  What stands in places that a token does
+ * not see, infinities and not-a-numbers too, does not reach its row.  Scores, sums and weighted
+ * values accumulate in fp32; the weights exp(s_p - running maximum) are rounded to the cache's type
+ * for their product with the values, their sum is not.  Results do not change from run to run. */
+size_t slimspec_tree_attention_workspace_bytes(const slimspec_cache *cache, const slimspec_batch *batch, int32_t q_heads);
+int slimspec_tree_attention(const slimspec_cache *cache, int32_t layer,
+                            const void *q, int32_t q_heads, int64_t q_token_stride, int64_t q_head_stride,
+                            const slimspec_batch *batch, const uint64_t *mask, int32_t mask_words, float scale,
+                            void *out, int64_t out_token_stride, int64_t out_head_stride, float *lse,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* The mask of drafted trees: bit j of mask[t] is set for t itself and for its ancestors.  parents
+ * [tokens]: the index in its own sequence of a token's parent, smaller than the token's, or -1 for
+ * a child of the committed context (so is a token whose parent is out of range).  mask [tokens, words],
+ * 1 <= words <= SLIMSPEC_TREE_MAX_WORDS; the rows of a sequence of more than 64 * words tokens are zero. */
+int slimspec_tree_mask(const int32_t *parents, const slimspec_batch *batch, int32_t words, uint64_t *mask, void *stream);
+
+/* Pages for the new tokens: every slot comes to hold the pages of lens + its new tokens.  The pages
+ * taken are the free ones of lowest number, in the order of the batch and of the places.  report
+ * (device, 1 entry): 0, or the number of pages that are lacking, or -1 where a sequence of the batch
+ * is not valid or needs more than slot_pages; then nothing has changed. */
+int slimspec_cache_reserve(const slimspec_cache *cache, const slimspec_batch *batch, int32_t *report, void *stream);
+
+/* Writes keys and values of the new tokens to their places, layers first_layer .. first_layer +
+ * n_layers - 1 at once: k_new, v_new [n_layers, tokens, heads, head_dim], with the strides given. */
+int slimspec_cache_append(const slimspec_cache *cache, int32_t first_layer, int32_t n_layers,
+                          const void *k_new, const void *v_new, int64_t new_layer_stride, int64_t new_token_stride, int64_t new_head_stride,
+                          const slimspec_batch *batch, void *stream);
+
+/* Moves an accepted path together, in place and in all layers: of sequence i the new tokens
+ * path[i][0] < path[i][1] < ... (accepted[i] of them, <= width; path [n, width]) go to places L, L + 1,
+ * ...  new_lens [n] (not the cache's lens) = L + accepted[i]; a path that is not increasing or not
+ * in the sequence's new tokens moves nothing, and new_lens[i] = L.  The cache's lens stay as they
+ * are: slimspec_cache_set_lens commits. */
+int slimspec_cache_compact(const slimspec_cache *cache, const slimspec_batch *batch,
+                           const int32_t *path, int32_t width, const int32_t *accepted, int32_t *new_lens, void *stream);
+
+/* Sets the committed lengths of n slots (lens [n], or null: 0, which frees the slots), at most what
+ * a slot's pages hold, and gives back the pages past them. */
+int slimspec_cache_set_lens(const slimspec_cache *cache, const int32_t *slots, int32_t n, const int32_t *lens, void *stream);
+
+/* Forks: slot children[i], which holds no pages, gets the committed tokens of slot parents[i]: its
+ * full pages shared, the last one, where it is not full, as a copy (all layers) in the free page of
+ * lowest number, in the order of i.  A parent may have several children; the children are distinct.
+ * report as for slimspec_cache_reserve (-1: a slot out of range, a child that holds pages, a parent
+ * that does not hold its own tokens' pages, or a child of itself). */
+int slimspec_cache_fork(const slimspec_cache *cache, const int32_t *parents, const int32_t *children, int32_t n,
+                        int32_t *report, void *stream);
 
 /* Human-readable name of a status code (static storage). */
 const char *slimspec_status_string(int status);

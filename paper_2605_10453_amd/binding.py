@@ -18,7 +18,11 @@ LIB_PATH = os.path.join(_HERE, "libslimspec.so")
 
 SLIMSPEC_BF16 = 0
 SLIMSPEC_F32 = 1
+SLIMSPEC_F16 = 2
 SLIMSPEC_KMAX = 64
+SLIMSPEC_CACHE_MAX_HEAD_DIM = 256
+SLIMSPEC_CACHE_MAX_SEQUENCES = 4096
+SLIMSPEC_TREE_MAX_WORDS = 64
 
 STATUS_OK = 0
 STATUS_INVALID_ARGUMENT = -1
@@ -30,12 +34,25 @@ STATIC_SCRATCH_BYTES = 64 << 20
 
 EXPORTED_SYMBOLS = (
     "slimspec_version", "slimspec_workspace_bytes", "slimspec_head_topk", "slimspec_transpose_weights", "slimspec_head_topk_prepared", "slimspec_head_topk_static", "full_head_topk", "truncated_head_topk", "slimspec_head_topk_positions", "slimspec_head_topk_positions_prepared", "slimspec_head_sample", "slimspec_head_sample_prepared", "full_head_sample", "routed_workspace_bytes", "routed_head_topk", "routed_head_topk_prepared",
+    "slimspec_tree_attention_workspace_bytes", "slimspec_tree_attention", "slimspec_tree_mask", "slimspec_cache_reserve", "slimspec_cache_append", "slimspec_cache_compact", "slimspec_cache_set_lens", "slimspec_cache_fork",
     "slimspec_status_string", "slimspec_last_hip_error", "slimspec_set_timing_events",
 )
 
 
 class SlimspecShape(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int32), ("d", ctypes.c_int32), ("r", ctypes.c_int32), ("V", ctypes.c_int32)]
+
+
+class SlimspecCache(ctypes.Structure):
+    _fields_ = ([(name, ctypes.c_void_p) for name in ("k", "v")]
+                + [(name, ctypes.c_int64) for name in ("layer_stride", "page_stride", "head_stride", "place_stride")]
+                + [(name, ctypes.c_void_p) for name in ("table", "held", "lens", "refs")]
+                + [(name, ctypes.c_int32) for name in ("layers", "pages", "heads", "page_size", "head_dim", "slots", "slot_pages")]
+                + [("dtype", ctypes.c_int)])
+
+
+class SlimspecBatch(ctypes.Structure):
+    _fields_ = [("slots", ctypes.c_void_p), ("first", ctypes.c_void_p), ("n", ctypes.c_int32), ("tokens", ctypes.c_int32)]
 
 
 class SlimspecError(RuntimeError):
@@ -91,6 +108,23 @@ def load_library() -> ctypes.CDLL:
     lib.routed_head_topk_prepared.argtypes = [vp, vp, vp, vp, vp, ctypes.c_int, shp, i32, i32, vp, vp, vp, sz, vp]
     lib.truncated_head_topk.restype = ctypes.c_int
     lib.truncated_head_topk.argtypes = [vp, vp, ctypes.c_int, vp, shp, i32, vp, vp, vp, sz, vp]
+    i64, cache, batch = ctypes.c_int64, ctypes.POINTER(SlimspecCache), ctypes.POINTER(SlimspecBatch)
+    lib.slimspec_tree_attention_workspace_bytes.restype = sz
+    lib.slimspec_tree_attention_workspace_bytes.argtypes = [cache, batch, i32]
+    lib.slimspec_tree_attention.restype = ctypes.c_int
+    lib.slimspec_tree_attention.argtypes = [cache, i32, vp, i32, i64, i64, batch, vp, i32, ctypes.c_float, vp, i64, i64, vp, vp, sz, vp]
+    lib.slimspec_tree_mask.restype = ctypes.c_int
+    lib.slimspec_tree_mask.argtypes = [vp, batch, i32, vp, vp]
+    lib.slimspec_cache_reserve.restype = ctypes.c_int
+    lib.slimspec_cache_reserve.argtypes = [cache, batch, vp, vp]
+    lib.slimspec_cache_append.restype = ctypes.c_int
+    lib.slimspec_cache_append.argtypes = [cache, i32, i32, vp, vp, i64, i64, i64, batch, vp]
+    lib.slimspec_cache_compact.restype = ctypes.c_int
+    lib.slimspec_cache_compact.argtypes = [cache, batch, vp, i32, vp, vp, vp]
+    lib.slimspec_cache_set_lens.restype = ctypes.c_int
+    lib.slimspec_cache_set_lens.argtypes = [cache, vp, i32, vp, vp]
+    lib.slimspec_cache_fork.restype = ctypes.c_int
+    lib.slimspec_cache_fork.argtypes = [cache, vp, vp, i32, vp, vp]
     lib.slimspec_status_string.restype = ctypes.c_char_p
     lib.slimspec_status_string.argtypes = [ctypes.c_int]
     lib.slimspec_last_hip_error.restype = ctypes.c_char_p
@@ -496,3 +530,201 @@ def routed_head_topk_prepared(h: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
     if st != STATUS_OK:
         _raise(st)
     return out_ids, out_logprobs
+
+
+# ---- drafted trees over a paged cache ----
+
+_CACHE_DTYPES = {torch.bfloat16: SLIMSPEC_BF16, torch.float16: SLIMSPEC_F16}
+
+
+def _int32_ptr(t: torch.Tensor, name: str, shape: tuple) -> int:
+    if t.dtype != torch.int32 or tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be int32 {list(shape)}")
+    return _dev_ptr(t, name)
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor that belongs to the stream of the call, so that its memory is not given to another stream's work while the call runs."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class PagedCache:
+    """A paged key/value cache: the caller's tensors, described once for the calls below.
+
+    k, v: [layers, pages, heads, page_size, head_dim] bf16 or fp16 device tensors of the same strides (the last one 1; a view
+    with heads and places in another order in memory will do).  table [slots, slot_pages], held [slots], lens [slots] and
+    refs [pages]: int32.  A cache starts with held, lens and refs zero.  The tensors are kept referenced and are written by
+    the calls; replacing a tensor takes a new PagedCache.
+    """
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, held: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor):
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v must be [layers, pages, heads, page_size, head_dim] tensors of the same strides and type")
+        if k.dtype not in _CACHE_DTYPES:
+            raise ValueError("a cache holds bfloat16 or float16")
+        if not k.is_cuda or not v.is_cuda:
+            raise ValueError("k and v must be device tensors")
+        if k.stride(4) != 1:
+            raise ValueError("the channels of a head must be adjacent")
+        if table.dim() != 2:
+            raise ValueError("table must be [slots, slot_pages]")
+        layers, pages, heads, page_size, head_dim = k.shape
+        slots, slot_pages = table.shape
+        self.k, self.v, self.table, self.held, self.lens, self.refs = k, v, table, held, lens, refs
+        self.layers, self.pages, self.heads, self.page_size, self.head_dim = layers, pages, heads, page_size, head_dim
+        self.slots, self.slot_pages, self.dtype, self.device = slots, slot_pages, k.dtype, k.device
+        self._struct = SlimspecCache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3),
+                                     _int32_ptr(table, "table", (slots, slot_pages)), _int32_ptr(held, "held", (slots,)),
+                                     _int32_ptr(lens, "lens", (slots,)), _int32_ptr(refs, "refs", (pages,)),
+                                     layers, pages, heads, page_size, head_dim, slots, slot_pages, _CACHE_DTYPES[k.dtype])
+        self._ref = ctypes.byref(self._struct)
+
+    @classmethod
+    def empty(cls, layers: int, pages: int, heads: int, page_size: int, head_dim: int, slots: int, slot_pages: int,
+              dtype: torch.dtype = torch.bfloat16, device="cuda") -> "PagedCache":
+        """A new cache without sequences."""
+        shape = (layers, pages, heads, page_size, head_dim)
+        k, v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        table, held, lens, refs = (torch.zeros(s, dtype=torch.int32, device=device) for s in ((slots, slot_pages), (slots,), (slots,), (pages,)))
+        return cls(k, v, table, held, lens, refs)
+
+
+def _batch(slots: torch.Tensor, first: torch.Tensor, tokens: int) -> SlimspecBatch:
+    n = slots.shape[0]
+    return SlimspecBatch(_int32_ptr(slots, "slots", (n,)), _int32_ptr(first, "first", (n + 1,)), n, tokens)
+
+
+def _check(st: int) -> None:
+    if st != STATUS_OK:
+        _raise(st)
+
+
+def tree_attention_workspace(cache: PagedCache, n: int, tokens: int, q_heads: int) -> torch.Tensor:
+    """Scratch for `tree_attention` calls of up to this many sequences and new tokens; calls that overlap in time need one each."""
+    need = load_library().slimspec_tree_attention_workspace_bytes(cache._ref, ctypes.byref(SlimspecBatch(None, None, n, tokens)), q_heads)
+    return torch.empty(max(int(need), 256), dtype=torch.uint8, device=cache.device)
+
+
+def tree_attention(cache: PagedCache, layer: int, q: torch.Tensor, slots: torch.Tensor, first: torch.Tensor,
+                   mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                   out: Optional[torch.Tensor] = None, lse=None, workspace: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Attention of drafted tokens over their sequences' caches, one layer: (out, lse).
+
+    q [tokens, q_heads, head_dim] in the cache's type, any strides that are multiples of 8 with adjacent channels; sequence i
+    lives in slot slots[i] (int32 [n]) and owns the tokens first[i] .. first[i + 1] - 1 (int32 [n + 1]), whose keys and values
+    `cache_append` has written behind the slot's committed tokens.  Every token sees the committed tokens and, of its
+    sequence's new ones, those of its row of mask (int64 [tokens, words], see `tree_mask`), or without a mask itself and the
+    ones before it.  scale: head_dim ** -0.5 unless given.  lse [tokens, q_heads] float32, or False: not asked for.
+    """
+    tokens, q_heads, head_dim = q.shape
+    if q.dtype != cache.dtype or head_dim != cache.head_dim or not q.is_cuda or q.stride(2) != 1:
+        raise ValueError("q must be a [tokens, q_heads, head_dim] device tensor of the cache's type and head_dim, its channels adjacent")
+    if out is None:
+        out = _empty((tokens, q_heads, head_dim), cache.dtype, cache.device, stream)
+    elif out.dtype != cache.dtype or out.shape != q.shape or not out.is_cuda or out.stride(2) != 1:
+        raise ValueError("out must be a device tensor of q's shape and type, its channels adjacent")
+    lse_ptr = None
+    if lse is False:
+        lse = None
+    else:
+        if lse is None:
+            lse = _empty((tokens, q_heads), torch.float32, cache.device, stream)
+        elif lse.dtype != torch.float32 or lse.shape != (tokens, q_heads):
+            raise ValueError("lse must be float32 [tokens, q_heads]")
+        lse_ptr = _dev_ptr(lse, "lse")
+    words, mask_ptr = 0, None
+    if mask is not None:
+        if mask.dtype != torch.int64 or mask.dim() != 2 or mask.shape[0] != tokens:
+            raise ValueError("mask must be int64 [tokens, words]")
+        words, mask_ptr = mask.shape[1], _dev_ptr(mask, "mask")
+    lib = load_library()
+    batch = ctypes.byref(_batch(slots, first, tokens))
+    if workspace is None:
+        workspace = _empty((max(int(lib.slimspec_tree_attention_workspace_bytes(cache._ref, batch, q_heads)), 256),), torch.uint8, cache.device, stream)
+    qs, os_ = q.stride(), out.stride()
+    _check(lib.slimspec_tree_attention(cache._ref, layer, q.data_ptr(), q_heads, qs[0], qs[1], batch, mask_ptr, words,
+                                       head_dim ** -0.5 if scale is None else scale, out.data_ptr(), os_[0], os_[1], lse_ptr,
+                                       _dev_ptr(workspace, "workspace"), workspace.nbytes, _stream_handle(stream)))
+    return out, lse
+
+
+def tree_mask(parents: torch.Tensor, first: torch.Tensor, words: int, out: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The mask [tokens, words] (int64 bit sets) of drafted trees from their parents (int32 [tokens], indices within the sequence, -1: none).
+
+    words: 64-bit words a row, enough for the longest sequence of the batch.
+    """
+    tokens, n = parents.shape[0], first.shape[0] - 1
+    if out is None:
+        out = _empty((tokens, words), torch.int64, parents.device, stream)
+    elif out.dtype != torch.int64 or tuple(out.shape) != (tokens, words):
+        raise ValueError("out must be int64 [tokens, words]")
+    batch = SlimspecBatch(None, _int32_ptr(first, "first", (n + 1,)), n, tokens)
+    _check(load_library().slimspec_tree_mask(_int32_ptr(parents, "parents", (tokens,)), ctypes.byref(batch), words, _dev_ptr(out, "out"), _stream_handle(stream)))
+    return out
+
+
+def cache_reserve(cache: PagedCache, slots: torch.Tensor, first: torch.Tensor, report: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Pages for a batch's new tokens (counts from `first`); report (int32 [1], device): 0, or the pages lacking, or -1; then nothing has changed."""
+    if report is None:
+        report = _empty((1,), torch.int32, cache.device, stream)
+    # the number of tokens is not needed here: the ranges in `first` are taken as they are
+    batch = _batch(slots, first, 0x7fffffff)
+    _check(load_library().slimspec_cache_reserve(cache._ref, ctypes.byref(batch), _int32_ptr(report, "report", (1,)), _stream_handle(stream)))
+    return report
+
+
+def cache_append(cache: PagedCache, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor, first: torch.Tensor,
+                 stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Writes the new tokens' keys and values ([tokens, heads, head_dim], or [n_layers, tokens, heads, head_dim] from `layer` on) to their places."""
+    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.dim() not in (3, 4):
+        raise ValueError("k_new and v_new must be [tokens, heads, head_dim] or [n_layers, tokens, heads, head_dim], with the same strides")
+    if k_new.dtype != cache.dtype or v_new.dtype != cache.dtype or not k_new.is_cuda or not v_new.is_cuda:
+        raise ValueError("k_new and v_new must be device tensors of the cache's type")
+    shape, strides = tuple(k_new.shape), k_new.stride()
+    if len(shape) == 3:
+        shape, strides = (1, *shape), (0, *strides)
+    if shape[2:] != (cache.heads, cache.head_dim) or strides[3] != 1:
+        raise ValueError("k_new and v_new must have the cache's heads and head_dim, their channels adjacent")
+    batch = _batch(slots, first, shape[1])
+    _check(load_library().slimspec_cache_append(cache._ref, layer, shape[0], k_new.data_ptr(), v_new.data_ptr(), *strides[:3],
+                                                ctypes.byref(batch), _stream_handle(stream)))
+
+
+def cache_compact(cache: PagedCache, slots: torch.Tensor, first: torch.Tensor, path: torch.Tensor, accepted: torch.Tensor,
+                  new_lens: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Moves accepted paths (int32 [n, width], increasing indices of new tokens; accepted [n] of them) together in all layers; the new lengths [n]."""
+    n = slots.shape[0]
+    if new_lens is None:
+        new_lens = _empty((n,), torch.int32, cache.device, stream)
+    if path.dim() != 2:
+        raise ValueError("path must be int32 [n, width]")
+    width = path.shape[1]
+    batch = _batch(slots, first, 0x7fffffff)
+    _check(load_library().slimspec_cache_compact(cache._ref, ctypes.byref(batch), _int32_ptr(path, "path", (n, width)), width,
+                                                 _int32_ptr(accepted, "accepted", (n,)), _int32_ptr(new_lens, "new_lens", (n,)), _stream_handle(stream)))
+    return new_lens
+
+
+def cache_set_lens(cache: PagedCache, slots: torch.Tensor, lens: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Sets the committed lengths of slots (None: 0, which frees them) and gives back the pages past them."""
+    n = slots.shape[0]
+    _check(load_library().slimspec_cache_set_lens(cache._ref, _int32_ptr(slots, "slots", (n,)), n,
+                                                  None if lens is None else _int32_ptr(lens, "lens", (n,)), _stream_handle(stream)))
+
+
+def cache_fork(cache: PagedCache, parents: torch.Tensor, children: torch.Tensor, report: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Slots children[i], which hold nothing, become forks of slots parents[i]; report as for `cache_reserve`."""
+    n = parents.shape[0]
+    if report is None:
+        report = _empty((1,), torch.int32, cache.device, stream)
+    _check(load_library().slimspec_cache_fork(cache._ref, _int32_ptr(parents, "parents", (n,)), _int32_ptr(children, "children", (n,)), n,
+                                              _int32_ptr(report, "report", (1,)), _stream_handle(stream)))
+    return report

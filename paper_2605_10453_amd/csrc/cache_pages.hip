@@ -1,0 +1,389 @@
+// The books and the rows of the paged cache: pages reserved, shared, copied and given back, rows written and moved together,
+// and the ancestor masks of drafted trees.
+//
+// A page is free when no slot holds it (refs = 0), and nothing else says so: there is no list of free pages whose order could
+// depend on which block gave its pages back first.  Giving back and sharing are commutative integer atomics on refs; taking is one
+// block that scans refs from page 0 on, so the pages taken are the lowest free ones whatever ran before, and a call's outcome is a
+// function of the books alone.
+#include "cache.hpp"
+
+namespace slimspec {
+namespace {
+
+constexpr int kBookThreads = 1024;
+
+// Exclusive sum of v over the block's threads; total: the sum.  `wave_sums`: kBookThreads / 64 ints of shared memory, free again when the call returns.
+__device__ __forceinline__ int block_scan(int v, int *wave_sums, int &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int inc = v;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int o = __shfl_up(inc, s);
+        if (lane >= s) inc += o;
+    }
+    if (lane == 63) wave_sums[wave] = inc;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kBookThreads / 64; ++w) {
+        const int x = wave_sums[w];
+        before += w < wave ? x : 0;
+        all += x;
+    }
+    __syncthreads();
+    total = all;
+    return before + inc - v;
+}
+
+// need[0 .. n) becomes its exclusive sum and need[n] the whole, which is returned; -1, and nothing is changed, where the whole passes 31 bits.
+__device__ int scan_needs(int *need, int n, int *wave_sums)
+{
+    __shared__ unsigned long long whole;
+    constexpr int kEach = kMaxSequences / kBookThreads;
+    const int at = threadIdx.x * kEach;
+    int mine[kEach];
+    unsigned long long sum = 0;
+    if (threadIdx.x == 0) whole = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        mine[j] = at + j < n ? need[at + j] : 0;
+        sum += mine[j];
+    }
+    if (sum) atomicAdd(&whole, sum);
+    __syncthreads();
+    if (whole > 0x7fffffff) return -1;
+    int total, before = block_scan((int)sum, wave_sums, total);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        if (at + j < n) need[at + j] = before;
+        before += mine[j];
+    }
+    if (threadIdx.x == 0) need[n] = total;
+    __syncthreads();
+    return total;
+}
+
+// Which of the n items page number `rank` of all that are wanted is for: the last i with start[i] <= rank.
+__device__ __forceinline__ int item_of(const int *start, int n, int rank)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= rank) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// Takes the `total` free pages of lowest number, in order: refs = 1, and entry(rank) of the table names the page.  Returns how many
+// there were; if too few, the ones taken are free again (the entries written stay: they are past what their slots hold).
+template <class Entry>
+__device__ int take_pages(const CacheView &c, int total, int *wave_sums, Entry entry)
+{
+    int taken = 0;
+    for (int base = 0; base < c.pages && taken < total; base += 4 * kBookThreads) {
+        const int p = base + 4 * threadIdx.x;
+        int4 r = make_int4(1, 1, 1, 1);
+        if (p + 4 <= c.pages) r = *reinterpret_cast<const int4 *>(c.refs + p);
+        else {
+            if (p < c.pages) r.x = c.refs[p];
+            if (p + 1 < c.pages) r.y = c.refs[p + 1];
+            if (p + 2 < c.pages) r.z = c.refs[p + 2];
+        }
+        const bool f[4] = {r.x == 0, r.y == 0, r.z == 0, r.w == 0};
+        int found;
+        int rank = taken + block_scan(f[0] + f[1] + f[2] + f[3], wave_sums, found);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (f[j]) {
+                if (rank < total) { *entry(rank) = p + j; c.refs[p + j] = 1; }
+                ++rank;
+            }
+        taken += found;
+    }
+    if (taken < total) {
+        __syncthreads();                          // the block's own writes of the entries
+        for (int r = threadIdx.x; r < taken; r += kBookThreads) c.refs[*entry(r)] = 0;
+    }
+    return taken;
+}
+
+__global__ __launch_bounds__(kBookThreads) void cache_reserve_kernel(CacheView c, BatchView b, int32_t *__restrict__ report)
+{
+    __shared__ int start[kMaxSequences + 1];
+    __shared__ int wave_sums[kBookThreads / 64];
+    bool bad = false;
+    for (int i = threadIdx.x; i < b.n; i += kBookThreads) {
+        const Sequence q = sequence_of(c, b, i);
+        const int want = (int)(((int64_t)q.len + q.tokens + (1 << c.page_shift) - 1) >> c.page_shift);
+        const int held = q.valid ? c.held[q.slot] : 0;
+        bad |= !q.valid || held < 0 || held > c.slot_pages;
+        start[i] = max(0, want - held);
+    }
+    if (__syncthreads_or(bad)) {
+        if (threadIdx.x == 0) *report = -1;
+        return;
+    }
+    const int total = scan_needs(start, b.n, wave_sums);
+    if (total < 0) {
+        if (threadIdx.x == 0) *report = 0x7fffffff;
+        return;
+    }
+    const int taken = take_pages(c, total, wave_sums, [&](int rank) {
+        const int i = item_of(start, b.n, rank), slot = b.slots[i];
+        return c.table + (int64_t)slot * c.slot_pages + c.held[slot] + (rank - start[i]);
+    });
+    if (taken >= total) {
+        __syncthreads();                          // the entries above were found by the old counts
+        for (int i = threadIdx.x; i < b.n; i += kBookThreads) {
+            const int need = start[i + 1] - start[i];
+            if (need > 0) c.held[b.slots[i]] += need;
+        }
+    }
+    if (threadIdx.x == 0) *report = total - min(taken, total);
+}
+
+// One block per slot: the pages past the new length lose a holder.
+__global__ __launch_bounds__(64) void cache_set_lens_kernel(CacheView c, const int32_t *__restrict__ slots, const int32_t *__restrict__ lens)
+{
+    const int i = blockIdx.x, slot = slots[i];
+    if (slot < 0 || slot >= c.slots) return;
+    const int held = min(max(c.held[slot], 0), c.slot_pages);
+    const int len = lens ? min(max(lens[i], 0), held << c.page_shift) : 0;
+    const int keep = (len + (1 << c.page_shift) - 1) >> c.page_shift;
+    for (int j = keep + (int)threadIdx.x; j < held; j += 64) {
+        const int page = c.table[(int64_t)slot * c.slot_pages + j];
+        if ((uint32_t)page < (uint32_t)c.pages) atomicSub(c.refs + page, 1);
+    }
+    if (threadIdx.x == 0) { c.held[slot] = keep; c.lens[slot] = len; }       // (one wavefront: every lane has read held)
+}
+
+// Fork, first launch: which pairs are valid, a free page for every child whose parent's last page is not full, the children's books.
+__global__ __launch_bounds__(kBookThreads) void cache_fork_books_kernel(CacheView c, const int32_t *__restrict__ parents, const int32_t *__restrict__ children,
+                                                                        int n, int32_t *__restrict__ report)
+{
+    __shared__ int start[kMaxSequences + 1];
+    __shared__ int wave_sums[kBookThreads / 64];
+    constexpr int kEach = kMaxSequences / kBookThreads;
+    int len[kEach];
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int i = threadIdx.x + j * kBookThreads;
+        len[j] = 0;
+        if (i >= n) continue;
+        const int p = parents[i], ch = children[i];
+        bool ok = p >= 0 && p < c.slots && ch >= 0 && ch < c.slots && p != ch;
+        if (ok) {
+            len[j] = c.lens[p];
+            const int held = c.held[p];
+            ok = len[j] >= 0 && held >= 0 && held <= c.slot_pages && len[j] <= (held << c.page_shift) && c.held[ch] == 0;
+        }
+        bad |= !ok;
+        start[i] = (len[j] & ((1 << c.page_shift) - 1)) ? 1 : 0;
+    }
+    if (__syncthreads_or(bad)) {
+        if (threadIdx.x == 0) *report = -1;
+        return;
+    }
+    const int total = scan_needs(start, n, wave_sums);
+    const int taken = take_pages(c, total, wave_sums, [&](int rank) {
+        const int i = item_of(start, n, rank);
+        return c.table + (int64_t)children[i] * c.slot_pages + (c.lens[parents[i]] >> c.page_shift);
+    });
+    if (taken >= total) {
+        __syncthreads();                          // the lengths above were the parents'
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int i = threadIdx.x + j * kBookThreads;
+            if (i >= n) continue;
+            c.lens[children[i]] = len[j];
+            c.held[children[i]] = (len[j] + (1 << c.page_shift) - 1) >> c.page_shift;
+        }
+    }
+    if (threadIdx.x == 0) *report = total - min(taken, total);
+}
+
+// Fork, second launch: block (pair, layer) copies the rows of the page that is not full; the blocks of layer 0 share the full pages.
+// (What the parent's books say is read from the child, which has them since the first launch.)
+__global__ __launch_bounds__(256) void cache_fork_rows_kernel(CacheView c, const int32_t *__restrict__ parents, const int32_t *__restrict__ children,
+                                                              const int32_t *__restrict__ report)
+{
+    if (*report != 0) return;
+    const int i = blockIdx.x, layer = blockIdx.y, p = parents[i], ch = children[i];
+    const int len = c.lens[ch], full = len >> c.page_shift, rest = len & ((1 << c.page_shift) - 1);
+    const int32_t *from = c.table + (int64_t)p * c.slot_pages;
+    int32_t *to = c.table + (int64_t)ch * c.slot_pages;
+    if (layer == 0)
+        for (int j = threadIdx.x; j < full; j += 256) {
+            const int page = from[j];
+            to[j] = page;
+            if ((uint32_t)page < (uint32_t)c.pages) atomicAdd(c.refs + page, 1);
+        }
+    if (rest == 0) return;
+    const int src = from[full], dst = to[full];
+    if ((uint32_t)src >= (uint32_t)c.pages || (uint32_t)dst >= (uint32_t)c.pages) return;
+    const int chunks = c.head_dim >> 3, per_head = rest * chunks;
+    const int64_t at = (int64_t)layer * c.layer_stride, a = at + src * c.page_stride, z = at + dst * c.page_stride;
+    for (int e = threadIdx.x; e < per_head * c.heads; e += 256) {
+        const int head = e / per_head, in = e - head * per_head, place = in / chunks, ck = in - place * chunks;
+        const int64_t o = head * c.head_stride + place * c.place_stride + 8 * ck;
+        const uint4 x = *reinterpret_cast<const uint4 *>(c.k + a + o), y = *reinterpret_cast<const uint4 *>(c.v + a + o);
+        *reinterpret_cast<uint4 *>(c.k + z + o) = x;
+        *reinterpret_cast<uint4 *>(c.v + z + o) = y;
+    }
+}
+
+// Block (token, layer): the row's keys and values to the token's place.
+__global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, int first_layer, NewRows rows, BatchView b)
+{
+    __shared__ int found;
+    if (threadIdx.x == 0) found = -1;
+    __syncthreads();
+    const int token = blockIdx.x;
+    for (int i = threadIdx.x; i < b.n; i += 256)
+        if (b.first[i] <= token && token < b.first[i + 1]) found = i;
+    __syncthreads();
+    if (found < 0) return;
+    const Sequence q = sequence_of(c, b, found);
+    if (!q.valid) return;
+    const int place = q.len + token - q.first, page = page_of(c, q.slot, place);
+    if (page < 0) return;
+    const int64_t to = (int64_t)(first_layer + blockIdx.y) * c.layer_stride + page * c.page_stride + (place & ((1 << c.page_shift) - 1)) * c.place_stride;
+    const int64_t from = (int64_t)blockIdx.y * rows.layer_stride + (int64_t)token * rows.token_stride;
+    const int chunks = c.head_dim >> 3;
+    for (int e = threadIdx.x; e < chunks * c.heads; e += 256) {
+        const int head = e / chunks, ck = e - head * chunks;
+        const uint4 x = *reinterpret_cast<const uint4 *>(rows.k + from + head * rows.head_stride + 8 * ck);
+        const uint4 y = *reinterpret_cast<const uint4 *>(rows.v + from + head * rows.head_stride + 8 * ck);
+        const int64_t o = to + head * c.head_stride + 8 * ck;
+        *reinterpret_cast<uint4 *>(c.k + o) = x;
+        *reinterpret_cast<uint4 *>(c.v + o) = y;
+    }
+}
+
+// Block (sequence, 256 columns of 16 bytes over layers, K and V, heads): a thread moves its column of all the path's rows, first to
+// last.  A row's place is never behind its source and the sources increase, so no row is overwritten before it has been read, with any
+// number of rows in flight; different threads' columns do not meet.
+constexpr int kPathBatch = 64, kMoveBatch = 8;
+__global__ __launch_bounds__(256) void cache_compact_kernel(CacheView c, BatchView b, const int32_t *__restrict__ path, int width,
+                                                            const int32_t *__restrict__ accepted, int32_t *__restrict__ new_lens)
+{
+    __shared__ int64_t src[kPathBatch], dst[kPathBatch];
+    const int i = blockIdx.y;
+    const Sequence q = sequence_of(c, b, i);
+    const int want = accepted[i];
+    const int32_t *p = path + (int64_t)i * width;
+    bool bad = !q.valid || want < 0 || want > width;
+    const int a = bad ? 0 : want;
+    for (int j = threadIdx.x; j < a; j += 256) {
+        const int x = p[j], before = j ? p[j - 1] : -1;
+        bad |= x <= before || x < 0 || x >= q.tokens;
+    }
+    bad = __syncthreads_or(bad);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        const int slot = b.slots[i];
+        new_lens[i] = bad ? (slot >= 0 && slot < c.slots ? c.lens[slot] : 0) : q.len + a;
+    }
+    if (bad) return;
+    const int chunks = c.head_dim >> 3, columns = 2 * c.layers * c.heads * chunks;
+    const int col = blockIdx.x * 256 + threadIdx.x;
+    const bool mine = col < columns;
+    const int ck = col % chunks, rest = col / chunks, head = rest % c.heads, lkv = rest / c.heads;
+    uint16_t *base = ((lkv & 1) ? c.v : c.k) + (int64_t)(lkv >> 1) * c.layer_stride + head * c.head_stride + 8 * ck;
+    const int in_page = (1 << c.page_shift) - 1;
+    for (int j0 = 0; j0 < a; j0 += kPathBatch) {
+        const int rows = min(kPathBatch, a - j0);
+        __syncthreads();
+        if ((int)threadIdx.x < rows) {
+            const int from = q.len + p[j0 + threadIdx.x], to = q.len + j0 + threadIdx.x;
+            const int fp = page_of(c, q.slot, from), tp = page_of(c, q.slot, to);
+            // a row that is in its place, or has no page, does not move
+            src[threadIdx.x] = from == to || fp < 0 || tp < 0 ? -1 : fp * c.page_stride + (from & in_page) * c.place_stride;
+            dst[threadIdx.x] = tp * c.page_stride + (to & in_page) * c.place_stride;
+        }
+        __syncthreads();
+        if (!mine) continue;
+        for (int r = 0; r < rows; r += kMoveBatch) {
+            uint4 x[kMoveBatch];
+#pragma unroll
+            for (int u = 0; u < kMoveBatch; ++u)
+                if (r + u < rows && src[r + u] >= 0) x[u] = *reinterpret_cast<const uint4 *>(base + src[r + u]);
+#pragma unroll
+            for (int u = 0; u < kMoveBatch; ++u)
+                if (r + u < rows && src[r + u] >= 0) *reinterpret_cast<uint4 *>(base + dst[r + u]) = x[u];
+        }
+    }
+}
+
+// Block per sequence, thread per token: the walk from a token to the root.  A parent's index is smaller than its child's, so the walk ends and
+// visits the mask's words from the last to the first: one word is held at a time.
+constexpr int kMaskThreads = 256;
+__global__ __launch_bounds__(kMaskThreads) void tree_mask_kernel(const int32_t *__restrict__ parents, BatchView b, int words, uint64_t *__restrict__ mask)
+{
+    __shared__ int up[64 * SLIMSPEC_TREE_MAX_WORDS];
+    const int lo = b.first[blockIdx.x], hi = b.first[blockIdx.x + 1];
+    if (lo < 0 || hi <= lo || hi > b.tokens) return;
+    const int tokens = hi - lo;
+    const bool fits = tokens <= 64 * words;
+    if (fits)
+        for (int t = threadIdx.x; t < tokens; t += kMaskThreads) {
+            const int p = parents[lo + t];
+            up[t] = p >= 0 && p < t ? p : -1;
+        }
+    __syncthreads();
+    for (int t = threadIdx.x; t < tokens; t += kMaskThreads) {
+        uint64_t *row = mask + (int64_t)(lo + t) * words;
+        int at = fits ? t : -1, w = words - 1;
+        while (w >= 0) {
+            uint64_t bits = 0;
+            while (at >= 64 * w) { bits |= (uint64_t)1 << (at & 63); at = up[at]; }
+            row[w--] = bits;
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_tree_mask(const int32_t *parents, const BatchView &b, int words, uint64_t *mask, hipStream_t st)
+{
+    tree_mask_kernel<<<b.n, kMaskThreads, 0, st>>>(parents, b, words, mask);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_reserve(const CacheView &c, const BatchView &b, int32_t *report, hipStream_t st)
+{
+    cache_reserve_kernel<<<1, kBookThreads, 0, st>>>(c, b, report);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_append(const CacheView &c, int first_layer, int n_layers, const NewRows &rows, const BatchView &b, hipStream_t st)
+{
+    cache_append_kernel<<<dim3(b.tokens, n_layers), 256, 0, st>>>(c, first_layer, rows, b);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_compact(const CacheView &c, const BatchView &b, const int32_t *path, int width, const int32_t *accepted, int32_t *new_lens, hipStream_t st)
+{
+    const int columns = 2 * c.layers * c.heads * (c.head_dim >> 3);
+    cache_compact_kernel<<<dim3((columns + 255) / 256, b.n), 256, 0, st>>>(c, b, path, width, accepted, new_lens);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_set_lens(const CacheView &c, const int32_t *slots, int n, const int32_t *lens, hipStream_t st)
+{
+    cache_set_lens_kernel<<<n, 64, 0, st>>>(c, slots, lens);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_fork(const CacheView &c, const int32_t *parents, const int32_t *children, int n, int32_t *report, hipStream_t st)
+{
+    cache_fork_books_kernel<<<1, kBookThreads, 0, st>>>(c, parents, children, n, report);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || n == 0) return e;
+    cache_fork_rows_kernel<<<dim3(n, c.layers), 256, 0, st>>>(c, parents, children, report);
+    return hipGetLastError();
+}
+
+}  // namespace slimspec

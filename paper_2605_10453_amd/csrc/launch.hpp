@@ -30,6 +30,9 @@ struct LdsLimit {
     std::mutex raising;
 };
 
+// Keeps the error's text for slimspec_last_hip_error (per host thread) and returns SLIMSPEC_HIP_ERROR.
+int fail_hip(hipError_t e);
+
 // slices of t = h A (fp32, [nds][R][r] with R = 1, 2, 4 or 8 >= rows_here) for up to kGemvMaxRows rows
 // A: a stack of [d, r] matrices; mat_of_row (host, rows_here entries, or null: matrix 0) names each row's
 hipError_t launch_down_projection(const uint16_t *h, const uint16_t *A, float *tpart,

@@ -19,8 +19,9 @@ std::atomic<void *> g_scratch_ptr[kMaxDevices] = {};      // device address of `
 
 thread_local char g_hip_error[256] = "";
 thread_local hipEvent_t g_ev_start = nullptr, g_ev_stop = nullptr;
+}  // namespace
 
-int fail_hip(hipError_t e)
+int slimspec::fail_hip(hipError_t e)
 {
     const char *s = hipGetErrorString(e);
     strncpy(g_hip_error, s ? s : "unknown HIP error", sizeof(g_hip_error) - 1);
@@ -28,6 +29,7 @@ int fail_hip(hipError_t e)
     return SLIMSPEC_HIP_ERROR;
 }
 
+namespace {
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Shape / k checks common to both heads.  Returns SLIMSPEC_OK or the error.

@@ -1,0 +1,368 @@
+"""Attention of drafted trees over a paged cache, against the definition in 64 bits."""
+import random
+
+import pytest
+import torch
+
+from cache_util import ancestor_sets, attention_bounds, attention_reference, mask_words
+
+pytestmark = pytest.mark.gpu
+BF, F16 = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2605_10453_amd import binding
+    return binding
+
+
+def make_cache(b, g, lens, counts, hkv, D, P, dtype, layers=1, places_outer=False, junk=1.0, pages_extra=3):
+    """A cache whose slots hold their pages in a shuffled order; every value drawn, those of no token too (times junk)."""
+    need = [-(-(x + t) // P) for x, t in zip(lens, counts)]
+    pages = sum(need) + pages_extra
+    kv = []
+    for _ in range(2):
+        shape = (layers, pages, P, hkv, D) if places_outer else (layers, pages, hkv, P, D)
+        x = (torch.randn(shape, generator=g) * junk).to(dtype).cuda()
+        kv.append(x.transpose(2, 3) if places_outer else x)
+    order = torch.randperm(pages, generator=g).tolist()
+    width = max(need + [1]) + 1
+    table = torch.full((len(lens), width), -5, dtype=torch.int32)
+    refs = torch.zeros(pages, dtype=torch.int32)
+    for i, m in enumerate(need):
+        for j in range(m):
+            table[i, j] = order.pop()
+            refs[table[i, j]] = 1
+    held = torch.tensor(need, dtype=torch.int32)
+    return b.PagedCache(kv[0], kv[1], table.cuda(), held.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), refs.cuda())
+
+
+def rows_of(cache, layer, slot, places):
+    """Keys and values [places, heads, D] of a slot, on the CPU in 64 bits."""
+    P = cache.page_size
+    place = torch.arange(places)
+    page = cache.table.cpu()[slot, place // P].long()
+    pick = lambda x: x[layer].cpu()[page, :, place % P].double()  # noqa: E731
+    return pick(cache.k), pick(cache.v)
+
+
+def check(b, cache, q, slots, counts, sets, scale, layer=0, mask=None, out=None, **kw):
+    """Runs the call and compares every row; sets: per sequence the new tokens that each token sees."""
+    first = [0]
+    for t in counts:
+        first.append(first[-1] + t)
+    dev = lambda xs: torch.tensor(xs, dtype=torch.int32, device="cuda")  # noqa: E731
+    got, lse = b.tree_attention(cache, layer, q, dev(slots), dev(first), mask=mask, scale=scale, out=out, **kw)
+    torch.cuda.synchronize()
+    got, lse, lens = got.cpu().double(), lse.cpu().double(), cache.lens.tolist()
+    G = q.shape[1] // cache.heads
+    qc = q.cpu().double()
+    for i, slot in enumerate(slots):
+        L, T = lens[slot], counts[i]
+        if T == 0:
+            continue
+        k, v = rows_of(cache, layer, slot, L + T)
+        seen = torch.zeros(T, L + T, dtype=torch.bool)
+        seen[:, :L] = True
+        for t in range(T):
+            for j in sets[i][t]:
+                seen[t, L + j] = True
+        for h in range(q.shape[1]):
+            ref = attention_reference(qc[first[i]:first[i + 1], h], k[:, h // G], v[:, h // G], seen, scale)
+            bound, bound_lse = attention_bounds(*ref, q.dtype)
+            o, e = got[first[i]:first[i + 1], h], lse[first[i]:first[i + 1], h]
+            empty = ~seen.any(1)
+            assert (o[empty] == 0).all() and (e[empty] == -float("inf")).all(), (i, h)
+            assert torch.isfinite(o).all(), (i, h, "not finite")
+            off = ((o - ref[0]).abs() / bound)
+            assert off.max() <= 1, (i, h, off.max().item(), off.argmax().item())
+            off = ((e - ref[1]).abs() / bound_lse)[~empty]
+            assert off.numel() == 0 or off.max() <= 1, (i, h, "lse", off.max().item())
+    return got, lse
+
+
+def chain(counts):
+    return [[set(range(t + 1)) for t in range(T)] for T in counts]
+
+
+def random_trees(rng, counts):
+    return [ancestor_sets([rng.randint(-1, t - 1) if t else -1 for t in range(T)]) for T in counts]
+
+
+SHAPES = [
+    # lens, counts, hq, hkv, D, P
+    ([0], [1], 1, 1, 64, 16),
+    ([1], [1], 8, 2, 128, 16),
+    ([15, 16, 17], [1, 1, 1], 8, 8, 128, 16),
+    ([500], [1], 32, 8, 128, 16),
+    ([3, 0, 250, 31], [5, 13, 1, 8], 10, 2, 80, 32),
+    ([63, 64, 65, 127, 128, 129], [1, 2, 3, 4, 5, 6], 4, 1, 64, 64),
+    ([700, 90], [17, 33], 8, 1, 128, 16),
+    ([300, 1000], [64, 40], 16, 2, 64, 32),
+    ([200], [130], 7, 1, 96, 128),
+    ([1500], [70], 14, 2, 256, 16),
+    ([40, 33], [3, 2], 3, 3, 8, 16),
+    ([100], [9], 5, 1, 72, 1024),
+    ([5000, 10, 2500], [2, 1, 7], 8, 4, 128, 256),
+    ([2000] * 5, [8] * 5, 8, 2, 120, 16),
+    ([90], [300], 4, 2, 64, 16),
+    ([0, 0], [257, 90], 2, 1, 128, 32),
+    ([33000], [3], 4, 1, 64, 64),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("tree", [True, False], ids=["tree", "chain"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, (len(s[0]), max(s[0]), max(s[1]), *s[2:]))))
+def test_matches_the_definition(b, shape, tree, dtype):
+    lens, counts, hq, hkv, D, P = shape
+    print("tree_attention", shape, tree, dtype, flush=True)
+    rng, g = random.Random(str(shape)), torch.Generator().manual_seed(len(lens) * 1000 + D)
+    cache = make_cache(b, g, lens, counts, hkv, D, P, dtype)
+    q = (torch.randn(sum(counts), hq, D, generator=g) * 1.5).to(dtype).cuda()
+    slots = list(range(len(lens)))
+    sets, mask = chain(counts), None
+    if tree:
+        sets = random_trees(rng, counts)
+        words = -(-max(counts) // 64)
+        mask = torch.cat([mask_words(s, words) for s in sets]).cuda()
+    check(b, cache, q, slots, counts, sets, D ** -0.5, mask=mask)
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+def test_order_of_slots_layers_strides(b, dtype):
+    """Sequences in other slots than their number, a second layer, places outside heads in memory, queries out of a wider row, an output with strides."""
+    g, rng = torch.Generator().manual_seed(5), random.Random(5)
+    lens, counts, hq, hkv, D = [70, 9, 300, 41], [6, 3, 0, 11], 12, 4, 128
+    by_slot = [lens[i] for i in (2, 0, 3, 1)]
+    count_by_slot = [counts[i] for i in (2, 0, 3, 1)]
+    cache = make_cache(b, g, by_slot, count_by_slot, hkv, D, 32, dtype, layers=3, places_outer=True)
+    slots = [1, 3, 0, 2]
+    wide = torch.randn(sum(counts), hq + 2 * hkv, D + 8, generator=g).to(dtype).cuda()
+    q = wide[:, hkv:hkv + hq, :D]
+    out = torch.full((sum(counts), hq + 1, D + 16), 7.0, dtype=dtype, device="cuda")
+    sets = random_trees(rng, counts)
+    mask = torch.cat([mask_words(s, 2) for s in sets]).cuda()
+    check(b, cache, q, slots, counts, sets, 0.11, layer=2, mask=mask, out=out[:, :hq, 8:8 + D])
+    assert (out[:, hq] == 7).all() and (out[:, :, :8] == 7).all() and (out[:, :, 8 + D:] == 7).all()
+
+
+@pytest.mark.parametrize("hq,hkv,D,counts,lens", [(4, 1, 64, [7, 20], [0, 37]), (8, 1, 128, [40, 3], [100, 0]), (64, 4, 80, [33, 65], [15, 300]),
+                                                  (8, 8, 256, [2, 5], [0, 1]), (32, 4, 128, [1, 1], [3, 700])])
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("bad", ["nan", "inf", "-inf"])
+def test_unseen_places_do_not_reach_a_row(b, hq, hkv, D, counts, lens, dtype, bad):
+    """Infinities and not-a-numbers in every place past a sequence's tokens and in new tokens that a row does not see; rows that see nothing of the tree."""
+    g, rng = torch.Generator().manual_seed(9), random.Random(9)
+    cache = make_cache(b, g, lens, counts, hkv, D, 16, dtype)
+    sets = random_trees(rng, counts)
+    # one token of each tree holds bad values and is seen by itself only, some rows see nothing new at all
+    rows = []
+    for i, s in enumerate(sets):
+        T, poison = counts[i], counts[i] // 2
+        for t in range(T):
+            s[t].discard(poison)
+        if T > 3:
+            s[T - 1] = set()
+            s[1] = set()
+        s[poison] = set()
+        rows.append(poison)
+    P = cache.page_size
+    used = torch.zeros(cache.pages, P, dtype=torch.bool)
+    table = cache.table.cpu()
+    for i, (L, T) in enumerate(zip(lens, counts)):
+        for place in range(L + T):
+            if place != L + rows[i]:
+                used[table[i, place // P], place % P] = True
+    clean_k, clean_v = cache.k.clone(), cache.v.clone()
+    at = (~used).nonzero().cuda()
+    for x in (cache.k, cache.v):
+        x[:, at[:, 0], :, at[:, 1]] = float(bad)
+    q = torch.randn(sum(counts), hq, D, generator=g).to(dtype).cuda()
+    mask = torch.cat([mask_words(s, -(-max(counts) // 64)) for s in sets]).cuda()
+    first = torch.tensor([0, counts[0], sum(counts)], dtype=torch.int32, device="cuda")
+    slots = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    got, lse = b.tree_attention(cache, 0, q, slots, first, mask=mask)
+    cache.k.copy_(clean_k)
+    cache.v.copy_(clean_v)
+    want, want_lse = check(b, cache, q, [0, 1], counts, sets, D ** -0.5, mask=mask)
+    assert torch.equal(got.cpu().double(), want) and torch.equal(lse.cpu().double(), want_lse)
+
+
+@pytest.mark.parametrize("T", [6, 90])
+def test_bad_values_that_a_row_sees_reach_that_row_only(b, T):
+    """A new token's value of infinity is seen by the token itself; every other row keeps what it has without it."""
+    g = torch.Generator().manual_seed(3)
+    D, lens, counts = 64, [50], [T]
+    cache = make_cache(b, g, lens, counts, 1, D, 16, BF)
+    sets = [[{t} for t in range(T)]]
+    mask = mask_words(sets[0], 2).cuda()
+    q = torch.randn(T, 4, D, generator=g).to(BF).cuda()
+    want, _ = check(b, cache, q, [0], counts, sets, D ** -0.5, mask=mask)
+    place = lens[0] + 3
+    page = cache.table.cpu()[0, place // 16]
+    cache.v[0, page, 0, place % 16, 5] = float("inf")
+    first = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    slots = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got, lse = b.tree_attention(cache, 0, q, slots, first, mask=mask)
+    got = got.cpu().double()
+    other = [t for t in range(T) if t != 3]
+    assert torch.equal(got[other], want[other])
+    assert (got[3, :, 5] == float("inf")).all()
+    keep = [c for c in range(D) if c != 5]
+    assert torch.equal(got[3][:, keep], want[3][:, keep])
+
+
+def test_large_scores(b):
+    """Scores of thousands, both signs, falling and rising along the context: the running maximum moves at every step, no weight overflows."""
+    g = torch.Generator().manual_seed(11)
+    D, L = 128, 900
+    for dtype, slope in ((BF, 1), (BF, -1), (F16, 1), (F16, -1)):
+        cache = make_cache(b, g, [L], [5], 1, D, 16, dtype)
+        table = cache.table.cpu()
+        for place in range(L):
+            cache.k[0, table[0, place // 16], 0, place % 16] *= (place if slope > 0 else L - place) / 40
+        q = (torch.randn(5, 8, D, generator=g) * 30).to(dtype).cuda()
+        check(b, cache, q, [0], [5], chain([5]), D ** -0.5)
+
+
+def test_missing_pages_and_sequences_out_of_range(b):
+    """What the device arrays hold wrong is left out: page numbers of no page, a slot and a token range that do not exist."""
+    g = torch.Generator().manual_seed(2)
+    D = 64
+    cache = make_cache(b, g, [100, 60], [4, 4], 2, D, 16, BF)
+    q = torch.randn(12, 4, D, generator=g).to(BF).cuda()
+    dev = lambda xs: torch.tensor(xs, dtype=torch.int32, device="cuda")  # noqa: E731
+    want, want_lse = b.tree_attention(cache, 0, q, dev([0, 1]), dev([0, 4, 8]))
+    # slot 7 does not exist; the sequence's rows stay as they are
+    out, lse = torch.full_like(q, 3.0), torch.full((12, 4), 3.0, device="cuda")
+    b.tree_attention(cache, 0, q, dev([0, 7, 1]), dev([0, 4, 4, 8]), out=out, lse=lse)
+    assert torch.equal(out[:8], want[:8]) and torch.equal(lse[:8], want_lse[:8]) and (out[8:] == 3).all()
+    out.fill_(3.0)
+    b.tree_attention(cache, 0, q, dev([0, 7, -1]), dev([0, 4, 8, 12]), out=out, lse=lse)
+    assert torch.equal(out[:4], want[:4]) and (out[4:] == 3).all()
+    out.fill_(3.0)
+    b.tree_attention(cache, 0, q, dev([0, 1]), dev([0, 4, 13]), out=out, lse=lse)
+    assert torch.equal(out[:4], want[:4]) and (out[4:] == 3).all()
+    out.fill_(3.0)
+    b.tree_attention(cache, 0, q, dev([0, 1]), dev([4, 0, 4]), out=out, lse=lse)      # a range that runs backwards, then slot 1 with rows 0 to 3
+    assert (out[4:] == 3).all()
+    # a page number out of range: its 16 places are seen by nobody
+    for wrong in (-1, cache.pages, 1 << 30):
+        cache.table[0, 2] = wrong
+        got, got_lse = b.tree_attention(cache, 0, q, dev([0]), dev([0, 4]))
+        assert torch.isfinite(got[:4]).all()
+        k, v = cache.k.cpu(), cache.v.cpu()
+        table = cache.table.cpu()
+        places = [p for p in range(104) if p // 16 != 2]
+        kk = torch.stack([k[0, table[0, p // 16], :, p % 16] for p in places]).double()
+        vv = torch.stack([v[0, table[0, p // 16], :, p % 16] for p in places]).double()
+        for h in range(4):
+            seen = torch.tensor([[p < 100 or p - 100 <= t for p in places] for t in range(4)])
+            ref = attention_reference(q.cpu().double()[:4, h], kk[:, h // 2], vv[:, h // 2], seen, D ** -0.5)
+            bound, bound_lse = attention_bounds(*ref, BF)
+            assert ((got.cpu().double()[:4, h] - ref[0]).abs() <= bound).all() and ((got_lse.cpu().double()[:4, h] - ref[1]).abs() <= bound_lse).all()
+    # a sequence none of whose pages exists sees nothing
+    cache.table[0].fill_(-1)
+    got, got_lse = b.tree_attention(cache, 0, q, dev([0]), dev([0, 4]))
+    assert (got[:4] == 0).all() and (got_lse[:4] == -float("inf")).all()
+    # a length that the table has no room for, and a negative one
+    for wrong in (10 ** 6, -3):
+        cache.lens[0] = wrong
+        out.fill_(3.0)
+        b.tree_attention(cache, 0, q, dev([0, 1]), dev([0, 4, 8]), out=out, lse=lse)
+        assert (out[:4] == 3).all() and torch.equal(out[4:8], want[4:8])
+
+
+def test_no_rows(b):
+    g = torch.Generator().manual_seed(2)
+    cache = make_cache(b, g, [10], [0], 2, 64, 16, BF)
+    q = torch.zeros(0, 4, 64, dtype=BF, device="cuda")
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = b.tree_attention(cache, 0, q, zero, torch.zeros(2, dtype=torch.int32, device="cuda"))
+    assert out.shape == (0, 4, 64) and lse.shape == (0, 4)
+    q = torch.zeros(3, 4, 64, dtype=BF, device="cuda")
+    out = torch.full_like(q, 2.0)
+    b.tree_attention(cache, 0, q, zero[:0], zero, out=out)
+    b.tree_attention(cache, 0, q, zero, torch.zeros(2, dtype=torch.int32, device="cuda"), out=out)
+    assert (out == 2).all()
+
+
+def test_many_sequences(b):
+    """More sequences than a block has threads, some without tokens."""
+    g, rng = torch.Generator().manual_seed(8), random.Random(8)
+    n = 700
+    lens, counts = [rng.randint(0, 90) for _ in range(n)], [rng.choice([0, 1, 1, 2, 5]) for _ in range(n)]
+    cache = make_cache(b, g, lens, counts, 1, 64, 16, BF)
+    q = torch.randn(sum(counts), 2, 64, generator=g).to(BF).cuda()
+    check(b, cache, q, list(range(n)), counts, chain(counts), 0.125)
+
+
+def test_same_results_every_time_and_on_other_streams(b):
+    g = torch.Generator().manual_seed(4)
+    lens, counts = [3000, 20, 999], [8, 8, 3]
+    cache = make_cache(b, g, lens, counts, 4, 128, 16, BF)
+    q = torch.randn(sum(counts), 16, 128, generator=g).to(BF).cuda()
+    dev = lambda xs: torch.tensor(xs, dtype=torch.int32, device="cuda")  # noqa: E731
+    slots, first = dev([0, 1, 2]), dev([0, 8, 16, 19])
+    ws = b.tree_attention_workspace(cache, 3, 19, 16)
+    want, want_lse = b.tree_attention(cache, 0, q, slots, first, workspace=ws)
+    for fill in (0x00, 0xAB, 0xFF):
+        ws.fill_(fill)
+        got, lse = b.tree_attention(cache, 0, q, slots, first, workspace=ws)
+        assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, lse = b.tree_attention(cache, 0, q, slots, first, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    got, none = b.tree_attention(cache, 0, q, slots, first, lse=False)
+    assert none is None and torch.equal(got, want)
+
+
+def test_in_a_graph_lengths_may_change(b):
+    """The lengths, tables and masks are read by the kernels: a captured call serves whatever they hold at the replay."""
+    g = torch.Generator().manual_seed(6)
+    lens, counts = [400, 77], [4, 4]
+    cache = make_cache(b, g, lens, counts, 2, 64, 16, F16)
+    q = torch.randn(8, 8, 64, generator=g).to(F16).cuda()
+    dev = lambda xs: torch.tensor(xs, dtype=torch.int32, device="cuda")  # noqa: E731
+    slots, first = dev([0, 1]), dev([0, 4, 8])
+    ws = b.tree_attention_workspace(cache, 2, 8, 8)
+    out, lse = torch.empty_like(q), torch.empty(8, 8, device="cuda")
+    b.tree_attention(cache, 0, q, slots, first, out=out, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.tree_attention(cache, 0, q, slots, first, out=out, lse=lse, workspace=ws)
+    for new in ([400, 77], [3, 60], [0, 0], [399, 1]):
+        cache.lens.copy_(dev(new))
+        want, want_lse = b.tree_attention(cache, 0, q, slots, first)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), new
+
+
+def test_offsets_beyond_32_bits(b):
+    """A pool of more than 2^32 elements, the sequence's pages at its end and in its middle."""
+    pages, P, D = 132000, 256, 128
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of free memory")
+    k, v = (torch.empty((1, pages, 1, P, D), dtype=BF, device="cuda") for _ in range(2))
+    assert k.numel() > 1 << 32
+    g = torch.Generator().manual_seed(1)
+    use = [pages - 1, 0, pages // 2, pages - 2]
+    for p in use:
+        k[0, p] = torch.randn(1, P, D, generator=g).to(BF).cuda()
+        v[0, p] = torch.randn(1, P, D, generator=g).to(BF).cuda()
+    dev = lambda xs: torch.tensor(xs, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = b.PagedCache(k, v, dev([use]), dev([4]), dev([1000]), torch.ones(pages, dtype=torch.int32, device="cuda"))
+    q = torch.randn(5, 4, D, generator=g).to(BF).cuda()
+    got, lse = b.tree_attention(cache, 0, q, dev([0]), dev([0, 5]))
+    kk, vv = (torch.cat([x[0, p, 0].cpu().double() for p in use])[:1005] for x in (k, v))
+    seen = torch.tensor([[p < 1000 or p - 1000 <= t for p in range(1005)] for t in range(5)])
+    for h in range(4):
+        ref = attention_reference(q.cpu().double()[:, h], kk, vv, seen, D ** -0.5)
+        bound, bound_lse = attention_bounds(*ref, BF)
+        assert ((got.cpu().double()[:, h] - ref[0]).abs() <= bound).all() and ((lse.cpu().double()[:, h] - ref[1]).abs() <= bound_lse).all()
