@@ -1,0 +1,322 @@
+// What the kernels of tree attention share: the matrix cores' operands, the weights of a step, and the division of the work.
+#pragma once
+#include "cache.hpp"
+#include "device_utils.hpp"
+
+namespace slimspec {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = 4;        // of a block
+constexpr int kStep = 32;                        // places per wavefront and step
+constexpr float kLowest = -3.0e38f;              // reference of a row without scores: finite, so that differences to it are numbers
+constexpr float kSlack = 8.f;                    // scores may pass the reference by this (in bits) before sums are scaled
+
+template <bool F16>
+__device__ __forceinline__ f32x4 mma(uint4 a, uint4 b, f32x4 c)
+{
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// two values rounded to the type (to nearest), the first one in the low half
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if constexpr (F16) return __builtin_bit_cast(uint32_t, (f16x2){(_Float16)a, (_Float16)b});
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
+}
+template <bool F16> __device__ __forceinline__ bool not_a_number_or_infinite(uint32_t half)
+{
+    constexpr uint32_t kExp = F16 ? 0x7c00u : 0x7f80u;
+    return (half & kExp) == kExp;
+}
+template <bool F16> __device__ __forceinline__ float value_of(uint16_t b)
+{
+    if constexpr (F16) return (float)__builtin_bit_cast(_Float16, b);
+    else return bf16_to_float(b);
+}
+
+// (largest over, sum over) the four lanes that hold a row: 16 and 32 away
+__device__ __forceinline__ float row_max(float v)
+{
+    uint32_t a, b;
+    swap_pair<16>(__float_as_uint(v), a, b);
+    v = fmaxf(__uint_as_float(a), __uint_as_float(b));
+    swap_pair<32>(__float_as_uint(v), a, b);
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ __forceinline__ float row_sum(float v)
+{
+    uint32_t a, b;
+    swap_pair<16>(__float_as_uint(v), a, b);
+    v = __uint_as_float(a) + __uint_as_float(b);
+    swap_pair<32>(__float_as_uint(v), a, b);
+    return __uint_as_float(a) + __uint_as_float(b);
+}
+
+// ---- the division of the work
+//
+// Units: one step of a block (32 WT places) for one row tile of one key head.  All units of a call, ordered by sequence, head, row tile
+// and place, are cut into equal runs, one per block, whatever the sequences' lengths; a run may begin and end inside a row tile, whose pieces
+// tree_merge_kernel joins.  The cut depends on the books alone, so results do not change from run to run.
+struct Division { int64_t units; int blocks; };
+__device__ __forceinline__ int64_t run_start(const Division &d, int block)
+{
+    if (d.units < 1 << 20) return (uint32_t)d.units * (uint32_t)block / (uint32_t)d.blocks;      // (fewer than 4096 blocks)
+    return d.units * block / d.blocks;
+}
+__device__ __forceinline__ int block_of(const Division &d, int64_t unit)
+{
+    if (d.units < 1 << 20) return (int)((((uint32_t)unit + 1) * (uint32_t)d.blocks - 1) / (uint32_t)d.units);
+    return (int)(((unit + 1) * d.blocks - 1) / d.units);
+}
+__device__ __forceinline__ int quotient(int64_t a, int b) { return a < 1ll << 31 ? (int)((uint32_t)a / (uint32_t)b) : (int)(a / b); }
+
+struct Tiling { int rows, places; };             // of a unit
+__device__ __forceinline__ int row_tiles(const Sequence &q, int group, const Tiling &t) { return (q.tokens * group + t.rows - 1) / t.rows; }
+__device__ __forceinline__ int steps_of(const Sequence &q, const Tiling &t) { return (int)(((int64_t)q.len + q.tokens + t.places - 1) / t.places); }
+__device__ __forceinline__ int64_t units_of(const CacheView &c, const Sequence &q, int group, const Tiling &t)
+{
+    return q.tokens ? (int64_t)row_tiles(q, group, t) * steps_of(q, t) * c.heads : 0;
+}
+
+// Workspace: the division and every sequence's share of it, for the merge; the pieces
+struct Share { int64_t start; int32_t steps, tiles; };                 // first unit; steps of a row tile; row tiles (0: nothing to do)
+struct TreePlan { int64_t units; int32_t blocks, pad; Share share[1]; };
+__host__ __device__ constexpr size_t plan_bytes(int n) { return ((size_t)16 + 16 * ((size_t)n + 1) + 255) & ~(size_t)255; }
+// a piece of a row tile: rows x DP sums, then the references and the weights' sums of the rows
+__host__ __device__ constexpr size_t piece_floats(int rows, int dp) { return (size_t)rows * dp + 2 * (size_t)rows; }
+
+__device__ __forceinline__ int64_t lane_value(int64_t v, int lane)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
+}
+// Inclusive sum over the wavefront's lanes: within rows of 16, then row 0 to row 1 and 2 to 3, then the lower half to the upper one.
+__device__ __forceinline__ int lanes_running_sum(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+    return v;
+}
+__device__ __forceinline__ int64_t lanes_running_sum(int64_t v)
+{
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+        const int64_t o = __shfl_up(v, s);
+        if ((int)(threadIdx.x & 63) >= s) v += o;
+    }
+    return v;
+}
+
+constexpr int kNear = 256;                       // the first so many sequences are kept in shared memory: a run that comes to its next one does not wait for two loads
+struct Run { int block; int64_t u, end; int seq; int64_t seq_start; Sequence s; };       // units [u, end) (none: u = end); the sequence of u and its first unit
+// A block's run.  Up to 64 sequences: every wavefront works it out by itself, a lane per sequence, without shared memory or a barrier; beyond,
+// the block's threads share the sequences.  Block 0 leaves the plan for the merge.
+__device__ __forceinline__ Run divide(const CacheView &c, const BatchView &b, int group, const Tiling &tile, Division &d, TreePlan *plan, int4 *near)
+{
+    __shared__ int64_t wave_sum[kWaves], found_start;
+    __shared__ int found;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool few = b.n <= kWave;
+    const int each = few ? 1 : (b.n + kThreads - 1) / kThreads, who = few ? lane : (int)threadIdx.x;
+    const int i0 = min(b.n, who * each), i1 = min(b.n, i0 + each);
+    Sequence s = {};
+    int64_t mine = 0;
+    for (int i = i0; i < i1; ++i) {
+        s = sequence_of(c, b, i);
+        mine += units_of(c, s, group, tile);
+        // (up to 64 sequences: every wavefront writes the same, and reads what it wrote itself)
+        if (i < kNear) near[i] = make_int4(s.slot, s.first, s.tokens, s.len);
+    }
+    int64_t inc;
+    if (__ballot(mine >= 1 << 24)) inc = lanes_running_sum(mine);
+    else inc = lanes_running_sum((int)mine);
+    int64_t total = lane_value(inc, 63), before = inc - mine;
+    if (!few) {
+        if (lane == 63) wave_sum[wave] = inc;
+        if (threadIdx.x == 0) { found = 0; found_start = 0; }
+        __syncthreads();
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) before += wave_sum[w];
+            total += wave_sum[w];
+        }
+    }
+    d.units = total;
+    d.blocks = (int)(total < (int64_t)gridDim.x ? (total > 0 ? total : 1) : gridDim.x);
+    if (blockIdx.x == 0 && (!few || wave == 0)) {
+        if (threadIdx.x == 0) { plan->units = total; plan->blocks = d.blocks; }
+        int64_t at = before;
+        for (int i = i0; i < i1; ++i) {
+            if (!few) s = sequence_of(c, b, i);
+            plan->share[i] = Share{at, steps_of(s, tile), s.tokens ? row_tiles(s, group, tile) : 0};
+            at += units_of(c, s, group, tile);
+        }
+    }
+    Run r;
+    r.block = blockIdx.x;
+    // blocks of one XCD (every eighth) take neighbouring runs: row tiles of the same keys meet in its L2
+    if (d.blocks == (int)gridDim.x && (gridDim.x & 7) == 0) r.block = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    r.u = r.end = 0;
+    r.seq = 0;
+    r.seq_start = 0;
+    if (total > 0 && r.block < d.blocks) {
+        r.u = run_start(d, r.block);
+        r.end = run_start(d, r.block + 1);
+    }
+    const bool here = mine > 0 && before <= r.u && r.u < before + mine;
+    if (few) {
+        const uint64_t hit = __ballot(here);
+        const int at = hit ? __ffsll((unsigned long long)hit) - 1 : 0;
+        r.seq = at;
+        r.seq_start = lane_value(before, at);
+        r.s = Sequence{__builtin_amdgcn_readlane(s.slot, at), __builtin_amdgcn_readlane(s.first, at), __builtin_amdgcn_readlane(s.tokens, at),
+                       __builtin_amdgcn_readlane(s.len, at), hit != 0};
+    } else {
+        if (here) {
+            int64_t at = before;
+            for (int i = i0; i < i1; ++i) {
+                const int64_t m = units_of(c, sequence_of(c, b, i), group, tile);
+                if (r.u < at + m) { found = i; found_start = at; break; }
+                at += m;
+            }
+        }
+        __syncthreads();
+        r.seq = __builtin_amdgcn_readfirstlane(found);
+        r.seq_start = lane_value(found_start, 0);
+        r.s = sequence_of(c, b, r.seq);
+    }
+    return r;
+}
+// A piece of the run: one row tile (head, rt) of a sequence, steps [step0, step1) of its `steps`.
+struct Piece { int slot, len, tokens, first, head, rt, step0, step1; bool whole; };
+__device__ __forceinline__ Piece next_piece(const CacheView &c, const BatchView &b, int group, const Tiling &tile, const int4 *near, Run &r)
+{
+    int64_t units = units_of(c, r.s, group, tile);
+    while (r.u >= r.seq_start + units) {
+        r.seq_start += units;
+        if (++r.seq < kNear) {
+            const int4 x = near[r.seq];
+            r.s = Sequence{__builtin_amdgcn_readfirstlane(x.x), __builtin_amdgcn_readfirstlane(x.y), __builtin_amdgcn_readfirstlane(x.z), __builtin_amdgcn_readfirstlane(x.w), true};
+        } else
+            r.s = sequence_of(c, b, r.seq);
+        units = units_of(c, r.s, group, tile);
+    }
+    Piece p;
+    p.slot = __builtin_amdgcn_readfirstlane(r.s.slot);
+    p.len = __builtin_amdgcn_readfirstlane(r.s.len);
+    p.tokens = __builtin_amdgcn_readfirstlane(r.s.tokens);
+    p.first = __builtin_amdgcn_readfirstlane(r.s.first);
+    const int steps = steps_of(r.s, tile), tiles = row_tiles(r.s, group, tile);
+    const int64_t rel = r.u - r.seq_start;
+    const int per_head = __builtin_amdgcn_readfirstlane(quotient(rel, steps));         // head * tiles + row tile
+    p.head = __builtin_amdgcn_readfirstlane(per_head / tiles);
+    p.rt = __builtin_amdgcn_readfirstlane(per_head - p.head * tiles);
+    p.step0 = __builtin_amdgcn_readfirstlane((int)(rel - (int64_t)per_head * steps));
+    const int64_t left = r.end - r.u;
+    p.step1 = __builtin_amdgcn_readfirstlane(left < steps - p.step0 ? p.step0 + (int)left : steps);
+    p.whole = p.step0 == 0 && p.step1 == steps;
+    r.u += p.step1 - p.step0;
+    return p;
+}
+
+// Which of a step's places p0 .. p0 + 31 a row sees.  there: those that are the sequence's and have a page (no_page: bit a for the
+// places 16 a .. 16 a + 15); row t of the sequence's new tokens.
+__device__ __forceinline__ uint32_t places_there(int p0, int end, uint32_t no_page)
+{
+    const int left = end - p0;
+    uint32_t there = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1 : 0u;
+    if (no_page & 1) there &= 0xffff0000u;
+    if (no_page & 2) there &= 0x0000ffffu;
+    return there;
+}
+__device__ __forceinline__ uint32_t places_seen(const TreeCall &call, int first, int t, int j0, uint32_t there)
+{
+    // j0: the new token that lies in the step's first place; negative: committed places come first
+    uint32_t w = 0;
+    if (call.mask) {
+        const uint64_t *words = call.mask + (int64_t)(first + t) * call.mask_words;
+        const int w0 = j0 >> 6, sh = j0 & 63;
+        const uint64_t lo = w0 >= 0 && w0 < call.mask_words ? words[w0] : 0;
+        const uint64_t hi = w0 + 1 >= 0 && w0 + 1 < call.mask_words ? words[w0 + 1] : 0;
+        w = (uint32_t)(lo >> sh) | (sh > 32 ? (uint32_t)(hi << (64 - sh)) : 0u);
+    } else {
+        const int k = t - j0;                                          // the last one that is seen
+        w = k >= 31 ? 0xffffffffu : k >= 0 ? (2u << k) - 1 : 0u;
+    }
+    if (j0 < 0) w |= j0 <= -32 ? 0xffffffffu : (1u << -j0) - 1;
+    return w & there;
+}
+
+// The weights of a step's 32 places for NQ tiles of 16 rows from their scores (S^T as the matrix cores leave it), rounded to the type in
+// pf; references m, sums l (of the lane's own places) and the accumulators o follow.
+template <bool F16, int NQ, int NO>
+__device__ __forceinline__ void weigh(f32x4 (&sc)[NQ][2], bool masked, const uint32_t (&seen)[NQ], int g, float unit, bool negative,
+                                      float (&m)[NQ], float (&l)[NQ], f32x4 (&o)[NQ][NO], uint4 (&pf)[NQ])
+{
+    if (negative) {
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) { sc[x][0] = -sc[x][0]; sc[x][1] = -sc[x][1]; }
+    }
+    if (masked) {
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(seen[x] >> (16 * a + 4 * g + i) & 1)) sc[x][a][i] = kNegInf;
+    }
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        float top = fmaxf(fmaxf(fmaxf(sc[x][0][0], sc[x][0][1]), fmaxf(sc[x][0][2], sc[x][0][3])),
+                          fmaxf(fmaxf(sc[x][1][0], sc[x][1][1]), fmaxf(sc[x][1][2], sc[x][1][3])));
+        top = row_max(top) * unit;
+        // (unseen everywhere: -infinity, which passes nothing)
+        const bool moves = top > m[x] + kSlack;
+        if (__ballot(moves)) {
+            const float to = moves ? top : m[x], f = __builtin_amdgcn_exp2f(m[x] - to);
+            m[x] = to;
+            l[x] *= f;
+#pragma unroll
+            for (int j = 0; j < NO; ++j) o[x][j] *= f;
+        }
+        float w[8];
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[4 * a + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x][a][i], unit, -m[x]));
+        l[x] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        pf[x] = make_uint4(pack2<F16>(w[0], w[1]), pack2<F16>(w[2], w[3]), pack2<F16>(w[4], w[5]), pack2<F16>(w[6], w[7]));
+    }
+}
+// Values of a masked step, as V^T's operand holds them (two places to a word, the ones of `there`'s bits n and n + 1): values of places
+// that are nobody's must not meet even a weight of zero; of new tokens, which some rows see and others do not, those that are no numbers or
+// infinite are left out here (returns whether there were any) and added to the rows that see them.
+template <bool F16>
+__device__ __forceinline__ bool leave_out(uint32_t &pair, uint32_t there, int n)
+{
+    uint32_t v = pair & ((there >> n & 1 ? 0x0000ffffu : 0u) | (there >> n & 2 ? 0xffff0000u : 0u));
+    const bool lo = not_a_number_or_infinite<F16>(v), hi = not_a_number_or_infinite<F16>(v >> 16);
+    pair = (lo ? 0u : v & 0x0000ffffu) | (hi ? 0u : v & 0xffff0000u);
+    return lo || hi;
+}
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }        // (a row that saw nothing has sums of zero)
+__device__ __forceinline__ float lse_of(float m, float sum) { return sum == 0.f ? kNegInf : (m + __builtin_amdgcn_logf(sum)) * kLn2; }
+
+// What a kernel over row tiles is given, and its launch
+struct TreeArgs { CacheView c; int layer; TreeCall call; BatchView b; TreePlan *plan; float *pieces; };
+// tree_tile.hip: head_dim padded to dp, 64 nq rows
+hipError_t launch_tree_tile(const TreeArgs &a, int nq, int blocks, hipStream_t st);
+
+}  // namespace slimspec
