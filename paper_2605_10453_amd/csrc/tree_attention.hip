@@ -28,7 +28,6 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
     const CacheView &c = args.c;
     const TreeCall &call = args.call;
     const BatchView &b = args.b;
-    const int layer = args.layer;
     float *const pieces = args.pieces;
     using Tile = TileOf<NQ, WR>;
     constexpr int kWT = Tile::kWT, kKC = DP / 32, kHalves = DP == 256 ? 2 : 1, kVW = DP == 64 ? 4 : 8;   // kVW: channels of V per lane and load
@@ -94,7 +93,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
     };
     auto offset_of = [&](const Piece &p, int step, int a, int of) {
         const int place = (step * kWT + wt) * kStep + 16 * a;
-        return (int64_t)layer * c.layer_stride + p.head * c.head_stride + (of < 0 ? 0 : of * c.page_stride + (place & in_page) * c.place_stride);
+        return p.head * c.head_stride + (of < 0 ? 0 : of * c.page_stride + (place & in_page) * c.place_stride);
     };
     auto load_k = [&](const Piece &p, int step, const int (&of)[2]) {
 #pragma unroll
@@ -190,16 +189,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
             bool odd_values = false;
             if (masked) {
 #pragma unroll
-                for (int n = 0; n < 8; n += 2)
+                for (int n = 0; n < 8; ++n)
 #pragma unroll
-                    for (int w = 0; w < kHalves * kVW / 2; ++w) {
-                        // (here a word holds two channels of one place: the same word of two places, turned)
-                        uint32_t lo = __builtin_amdgcn_perm(vf[n + 1][w], vf[n][w], 0x05040100u), hi = __builtin_amdgcn_perm(vf[n + 1][w], vf[n][w], 0x07060302u);
-                        odd_values |= leave_out<F16>(lo, there, 16 * (n >> 2) + 4 * g + (n & 3));
-                        odd_values |= leave_out<F16>(hi, there, 16 * (n >> 2) + 4 * g + (n & 3));
-                        vf[n][w] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
-                        vf[n + 1][w] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-                    }
+                    for (int w = 0; w < kHalves * kVW / 2; ++w) odd_values |= leave_out<F16>(vf[n][w], there >> (16 * (n >> 2) + 4 * g + (n & 3)) & 1);
             }
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
@@ -323,56 +315,55 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
     }
 }
 
-// Joins the pieces of the row tiles that more than one block worked on.  WPR wavefronts per query row; DP / 4 lanes hold a piece's row,
-// so a wavefront goes over 256 / DP pieces at a time, and the partial sums meet across lanes and, WPR = 4, in shared memory.
-template <bool F16, int DP, int WPR>
-__global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeArgs args, Tiling tile)
+// What is left of a row tile cut into pieces [b0, b1] (named by their blocks): where a piece's numbers are.  The first piece is its block's
+// second one, unless the block began with it.
+__device__ __forceinline__ const float *piece_at(const float *pieces, size_t stride, int k, int b0, bool second)
+{
+    return pieces + ((size_t)2 * k + (k == b0 && second ? 1 : 0)) * stride;
+}
+
+// Joins the pieces of the row tiles that more than one block worked on.  For few rows, of which one long sequence has up to 96 pieces each:
+// a block per query row.  DP / 4 lanes hold a piece's row, so that the block goes over 1024 / DP pieces at a time; the partial sums meet across
+// lanes and in shared memory.
+template <bool F16, int DP>
+__global__ __launch_bounds__(kThreads) void tree_merge_rows_kernel(TreeArgs args, Tiling tile)
 {
     const CacheView &c = args.c;
     const TreeCall &call = args.call;
     const BatchView &b = args.b;
-    const TreePlan *const plan = args.plan;
-    const float *const pieces = args.pieces;
     constexpr int kLanes = DP / 4, kPieces = kWave / kLanes;
-    __shared__ __align__(16) float joint[WPR > 1 ? kWaves * (DP + 2) : 4];
+    __shared__ __align__(16) float joint[kWaves * (DP + 2)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = call.q_heads / c.heads;
-    const int64_t index = WPR > 1 ? blockIdx.x : (int64_t)blockIdx.x * kWaves + wave;
-    if (index >= (int64_t)b.tokens * call.q_heads) return;
-    const int token = quotient(index, call.q_heads), qh = (int)(index - (int64_t)token * call.q_heads);
-    Division div{plan->units, plan->blocks};
-    int first = 0;
+    const int token = blockIdx.x / call.q_heads, qh = blockIdx.x - token * call.q_heads;
+    Division div{args.plan->units, args.plan->blocks};
     Share sh = {};
     bool hit = false;
     for (int i0 = 0; i0 < b.n; i0 += kWave) {
-        const int i = min(i0 + lane, b.n - 1);
-        const int lo = b.first[i], hi = b.first[i + 1];
-        const Share x = plan->share[i];
-        const uint64_t here = __ballot(i0 + lane < b.n && lo <= token && token < hi && x.tiles > 0);
+        const Share x = args.plan->share[min(i0 + lane, b.n - 1)];
+        const uint64_t here = __ballot(i0 + lane < b.n && x.tiles > 0 && x.first <= token && token - x.first < x.tokens);
         if (!here) continue;
         const int at = __ffsll((unsigned long long)here) - 1;
         hit = true;
-        first = __builtin_amdgcn_readlane(lo, at);
-        sh = Share{lane_value(x.start, at), __builtin_amdgcn_readlane(x.steps, at), __builtin_amdgcn_readlane(x.tiles, at)};
+        sh = Share{lane_value(x.start, at), __builtin_amdgcn_readlane(x.steps, at), __builtin_amdgcn_readlane(x.tiles, at), __builtin_amdgcn_readlane(x.first, at), 0};
         break;
     }
     if (!hit) return;
-    const int head = qh / group, row = (token - first) * group + qh - head * group, rt = row / tile.rows, in = row - rt * tile.rows;
+    const int head = qh / group, row = (token - sh.first) * group + qh - head * group, rt = row / tile.rows, in = row - rt * tile.rows;
     const int64_t u0 = sh.start + ((int64_t)head * sh.tiles + rt) * sh.steps;
     const int b0 = block_of(div, u0), b1 = block_of(div, u0 + sh.steps - 1);
     if (b0 == b1) return;
-    const bool second = run_start(div, b0) != u0;                      // the first piece is its block's second one
+    const bool second = run_start(div, b0) != u0;
     const size_t stride = piece_floats(tile.rows, DP);
     const int d = 4 * (lane % kLanes);
     float m = kLowest, sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    constexpr int kAhead = 4, kApart = kPieces * WPR;
-    for (int k0 = b0 + (WPR > 1 ? wave * kPieces : 0) + lane / kLanes; k0 <= b1; k0 += kAhead * kApart) {
+    constexpr int kAhead = 4, kApart = kPieces * kWaves;
+    for (int k0 = b0 + wave * kPieces + lane / kLanes; k0 <= b1; k0 += kAhead * kApart) {
         float mk[kAhead], lk[kAhead];
         f32x4 ok[kAhead];
 #pragma unroll
         for (int x = 0; x < kAhead; ++x) {
-            const int k = k0 + x * kApart;
-            const float *from = pieces + ((size_t)2 * min(k, b1) + (k == b0 && second ? 1 : 0)) * stride;
+            const float *from = piece_at(args.pieces, stride, min(k0 + x * kApart, b1), b0, second);
             mk[x] = from[(size_t)tile.rows * DP + in];
             lk[x] = from[(size_t)tile.rows * (DP + 1) + in];
             ok[x] = *reinterpret_cast<const f32x4 *>(from + (size_t)in * DP + d);
@@ -405,22 +396,87 @@ __global__ __launch_bounds__(kThreads) void tree_merge_kernel(TreeArgs args, Til
         for (int n = 0; n < 4; ++n) o2[n] = __shfl_xor(o[n], s);
         join(__shfl_xor(m, s), __shfl_xor(sum, s), o2);
     }
-    if constexpr (WPR > 1) {
-        if (lane < kLanes) {
-            *reinterpret_cast<f32x4 *>(joint + wave * DP + d) = o;
-            if (lane == 0) { joint[kWaves * DP + wave] = m; joint[kWaves * (DP + 1) + wave] = sum; }
-        }
-        __syncthreads();
-        if (wave != 0) return;
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) join(joint[kWaves * DP + w], joint[kWaves * (DP + 1) + w], *reinterpret_cast<const f32x4 *>(joint + w * DP + d));
+    if (lane < kLanes) {
+        *reinterpret_cast<f32x4 *>(joint + wave * DP + d) = o;
+        if (lane == 0) { joint[kWaves * DP + wave] = m; joint[kWaves * (DP + 1) + wave] = sum; }
     }
-    if (lane >= kLanes) return;
+    __syncthreads();
+    if (wave != 0 || lane >= kLanes) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) join(joint[kWaves * DP + w], joint[kWaves * (DP + 1) + w], *reinterpret_cast<const f32x4 *>(joint + w * DP + d));
     const float inv = inverse(sum);
     if (d < c.head_dim)
         *reinterpret_cast<uint2 *>(call.out + (int64_t)token * call.out_token_stride + (int64_t)qh * call.out_head_stride + d) =
             make_uint2(pack2<F16>(o[0] * inv, o[1] * inv), pack2<F16>(o[2] * inv, o[3] * inv));
     if (call.lse && lane == 0) call.lse[(int64_t)token * call.q_heads + qh] = lse_of(m, sum);
+}
+
+// ... for many rows: block (k, y) of the launch looks at the boundary between the runs k and k + 1; if it is the first one inside its row tile,
+// the blocks (k, *) join the tile, four lots of four channels to a thread.
+constexpr int kLots = 4;
+template <bool F16, int DP>
+__global__ __launch_bounds__(kThreads) void tree_merge_tiles_kernel(TreeArgs args, Tiling tile)
+{
+    const CacheView &c = args.c;
+    const TreeCall &call = args.call;
+    const int lane = threadIdx.x & 63, group = call.q_heads / c.heads;
+    Division div{args.plan->units, args.plan->blocks};
+    const int next = blockIdx.x + 1;
+    if (next >= div.blocks) return;
+    const int64_t u = run_start(div, next);
+    Share sh = {};
+    for (int i0 = 0; i0 < args.b.n; i0 += kWave) {
+        const Share x = args.plan->share[min(i0 + lane, args.b.n - 1)];
+        const uint64_t here = __ballot(i0 + lane < args.b.n && x.start <= u && u - x.start < (int64_t)x.steps * x.tiles * c.heads);
+        if (!here) continue;
+        const int at = __ffsll((unsigned long long)here) - 1;
+        sh = Share{lane_value(x.start, at), __builtin_amdgcn_readlane(x.steps, at), __builtin_amdgcn_readlane(x.tiles, at), __builtin_amdgcn_readlane(x.first, at),
+                   __builtin_amdgcn_readlane(x.tokens, at)};
+        break;
+    }
+    if (sh.steps == 0) return;
+    const int per_head = quotient(u - sh.start, sh.steps);             // head * tiles + row tile
+    const int64_t u0 = sh.start + (int64_t)per_head * sh.steps;
+    if (u == u0 || block_of(div, u0) != (int)blockIdx.x) return;
+    const int b0 = blockIdx.x, b1 = block_of(div, u0 + sh.steps - 1), head = per_head / sh.tiles, rt = per_head - head * sh.tiles;
+    const bool second = run_start(div, b0) != u0;
+    const size_t stride = piece_floats(tile.rows, DP);
+    const int rows = min(tile.rows, sh.tokens * group - rt * tile.rows);
+    int in[kLots], d[kLots];
+    float m[kLots], sum[kLots];
+    f32x4 o[kLots];
+#pragma unroll
+    for (int x = 0; x < kLots; ++x) {
+        const int e = (blockIdx.y * kLots + x) * kThreads + threadIdx.x;
+        in[x] = e / (DP / 4);
+        d[x] = 4 * (e % (DP / 4));
+        m[x] = kLowest;
+        sum[x] = 0.f;
+        o[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll 2
+    for (int k = b0; k <= b1; ++k) {
+        const float *from = piece_at(args.pieces, stride, k, b0, second);
+#pragma unroll
+        for (int x = 0; x < kLots; ++x) {
+            const int i = min(in[x], rows - 1);
+            const float mk = from[(size_t)tile.rows * DP + i], lk = from[(size_t)tile.rows * (DP + 1) + i];
+            const f32x4 ok = *reinterpret_cast<const f32x4 *>(from + (size_t)i * DP + d[x]);
+            const float to = fmaxf(m[x], mk), f = __builtin_amdgcn_exp2f(m[x] - to), f2 = __builtin_amdgcn_exp2f(mk - to);
+            m[x] = to;
+            sum[x] = sum[x] * f + lk * f2;
+            o[x] = o[x] * f + ok * f2;
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < kLots; ++x) {
+        if (in[x] >= rows || d[x] >= c.head_dim) continue;
+        const int row = rt * tile.rows + in[x], t = row / group, token = sh.first + t, qh = head * group + row - t * group;
+        const float inv = inverse(sum[x]);
+        *reinterpret_cast<uint2 *>(call.out + (int64_t)token * call.out_token_stride + (int64_t)qh * call.out_head_stride + d[x]) =
+            make_uint2(pack2<F16>(o[x][0] * inv, o[x][1] * inv), pack2<F16>(o[x][2] * inv, o[x][3] * inv));
+        if (call.lse && d[x] == 0) call.lse[(int64_t)token * call.q_heads + qh] = lse_of(m[x], sum[x]);
+    }
 }
 
 // ---- the host's side: which tiling, how many blocks
@@ -450,12 +506,15 @@ Choice choose(int n, int tokens, int group, int head_dim)
 }
 
 template <bool F16, int DP>
-hipError_t merge(const TreeArgs &a, const Tiling &tile, hipStream_t st)
+hipError_t merge(const TreeArgs &a, const Choice &k, hipStream_t st)
 {
     const int64_t rows = (int64_t)a.b.tokens * a.call.q_heads;
-    // few rows of many pieces each (one long sequence: up to 96): a block per row
-    if (rows <= 2048) tree_merge_kernel<F16, DP, 4><<<(unsigned)rows, kThreads, 0, st>>>(a, tile);
-    else tree_merge_kernel<F16, DP, 1><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, st>>>(a, tile);
+    const Tiling tile{k.rows, k.places};
+    if (rows <= 2048) tree_merge_rows_kernel<F16, DP><<<(unsigned)rows, kThreads, 0, st>>>(a, tile);
+    else {
+        const int lots = k.rows * (DP / 4), per_block = kLots * kThreads;
+        tree_merge_tiles_kernel<F16, DP><<<dim3(k.blocks - 1, (lots + per_block - 1) / per_block), kThreads, 0, st>>>(a, tile);
+    }
     return hipGetLastError();
 }
 
@@ -479,7 +538,7 @@ hipError_t launch(const TreeArgs &a, const Choice &k, hipStream_t st)
 {
     const hipError_t e = k.tile ? launch_tree_tile(a, k.nq, k.blocks, st)
                        : a.c.head_dim == DP ? launch_rows<F16, DP, true>(a, k, st) : launch_rows<F16, DP, false>(a, k, st);
-    return e != hipSuccess ? e : merge<F16, DP>(a, Tiling{k.rows, k.places}, st);
+    return e != hipSuccess ? e : merge<F16, DP>(a, k, st);
 }
 
 template <bool F16>
@@ -509,7 +568,10 @@ size_t tree_attention_workspace_bytes(int n, int tokens, int q_heads, int heads,
 
 hipError_t launch_tree_attention(const CacheView &c, int layer, const TreeCall &call, const BatchView &b, void *workspace, hipStream_t st)
 {
-    const TreeArgs a{c, layer, call, b, static_cast<TreePlan *>(workspace), reinterpret_cast<float *>(static_cast<char *>(workspace) + plan_bytes(b.n))};
+    CacheView at = c;
+    at.k += layer * c.layer_stride;
+    at.v += layer * c.layer_stride;
+    const TreeArgs a{at, call, b, static_cast<TreePlan *>(workspace), reinterpret_cast<float *>(static_cast<char *>(workspace) + plan_bytes(b.n))};
     const Choice k = choose(b.n, b.tokens, call.q_heads / c.heads, c.head_dim);
     return call.f16 ? launch_type<true>(a, k, st) : launch_type<false>(a, k, st);
 }

@@ -86,9 +86,9 @@ __device__ __forceinline__ int64_t units_of(const CacheView &c, const Sequence &
 }
 
 // Workspace: the division and every sequence's share of it, for the merge; the pieces
-struct Share { int64_t start; int32_t steps, tiles; };                 // first unit; steps of a row tile; row tiles (0: nothing to do)
+struct Share { int64_t start; int32_t steps, tiles, first, tokens; };  // first unit; steps of a row tile; row tiles (0: nothing to do); its tokens
 struct TreePlan { int64_t units; int32_t blocks, pad; Share share[1]; };
-__host__ __device__ constexpr size_t plan_bytes(int n) { return ((size_t)16 + 16 * ((size_t)n + 1) + 255) & ~(size_t)255; }
+__host__ __device__ constexpr size_t plan_bytes(int n) { return ((size_t)16 + 24 * ((size_t)n + 1) + 255) & ~(size_t)255; }
 // a piece of a row tile: rows x DP sums, then the references and the weights' sums of the rows
 __host__ __device__ constexpr size_t piece_floats(int rows, int dp) { return (size_t)rows * dp + 2 * (size_t)rows; }
 
@@ -159,7 +159,7 @@ __device__ __forceinline__ Run divide(const CacheView &c, const BatchView &b, in
         int64_t at = before;
         for (int i = i0; i < i1; ++i) {
             if (!few) s = sequence_of(c, b, i);
-            plan->share[i] = Share{at, steps_of(s, tile), s.tokens ? row_tiles(s, group, tile) : 0};
+            plan->share[i] = Share{at, steps_of(s, tile), s.tokens ? row_tiles(s, group, tile) : 0, s.first, s.tokens};
             at += units_of(c, s, group, tile);
         }
     }
@@ -300,13 +300,13 @@ __device__ __forceinline__ void weigh(f32x4 (&sc)[NQ][2], bool masked, const uin
         pf[x] = make_uint4(pack2<F16>(w[0], w[1]), pack2<F16>(w[2], w[3]), pack2<F16>(w[4], w[5]), pack2<F16>(w[6], w[7]));
     }
 }
-// Values of a masked step, as V^T's operand holds them (two places to a word, the ones of `there`'s bits n and n + 1): values of places
-// that are nobody's must not meet even a weight of zero; of new tokens, which some rows see and others do not, those that are no numbers or
-// infinite are left out here (returns whether there were any) and added to the rows that see them.
+// Two values of a place in a masked step: values of places that are nobody's must not meet even a weight of zero; of new tokens, which some
+// rows see and others do not, those that are no numbers or infinite are left out here (returns whether there were any) and added to the rows
+// that see them.
 template <bool F16>
-__device__ __forceinline__ bool leave_out(uint32_t &pair, uint32_t there, int n)
+__device__ __forceinline__ bool leave_out(uint32_t &pair, bool there)
 {
-    uint32_t v = pair & ((there >> n & 1 ? 0x0000ffffu : 0u) | (there >> n & 2 ? 0xffff0000u : 0u));
+    const uint32_t v = there ? pair : 0u;
     const bool lo = not_a_number_or_infinite<F16>(v), hi = not_a_number_or_infinite<F16>(v >> 16);
     pair = (lo ? 0u : v & 0x0000ffffu) | (hi ? 0u : v & 0xffff0000u);
     return lo || hi;
@@ -315,7 +315,8 @@ __device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 
 __device__ __forceinline__ float lse_of(float m, float sum) { return sum == 0.f ? kNegInf : (m + __builtin_amdgcn_logf(sum)) * kLn2; }
 
 // What a kernel over row tiles is given, and its launch
-struct TreeArgs { CacheView c; int layer; TreeCall call; BatchView b; TreePlan *plan; float *pieces; };
+// (c.k and c.v point at the layer)
+struct TreeArgs { CacheView c; TreeCall call; BatchView b; TreePlan *plan; float *pieces; };
 // tree_tile.hip: head_dim padded to dp, 64 nq rows
 hipError_t launch_tree_tile(const TreeArgs &a, int nq, int blocks, hipStream_t st);
 

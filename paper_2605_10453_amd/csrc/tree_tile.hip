@@ -10,6 +10,7 @@
 // whatever is left to do, and vector memory returns in order: s_waitcnt vmcnt((NBUF - 2) LPS) = its part of the stage needed next has
 // landed (other loads and stores only make the wait longer); the barrier then says so for all, and that all have read the stage before.
 #include "tree_parts.hpp"
+#include <type_traits>
 
 namespace slimspec {
 namespace {
@@ -41,6 +42,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
     constexpr int kKC = DP / 32, kO = DP / 16, kRows = 64 * NQ;
     __shared__ __align__(1024) unsigned char stages[S::kBufs * S::kBytes];
     __shared__ int4 near[kNear];
+    __shared__ int odd_in;                                             // the last masked step (counted from 1) with values left out
     const CacheView &c = args.c;
     const TreeCall &call = args.call;
     const BatchView &b = args.b;
@@ -54,8 +56,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int D = EXACT ? DP : c.head_dim;
     const int in_page = (1 << c.page_shift) - 1;
-    const float unit = fmaxf(fabsf(call.scale) * kLog2e, 1.2e-38f);    // (not 0: an unseen place's score of -infinity stays one)
-    const bool negative = call.scale < 0.f;
+    const float scaled = call.scale * kLog2e, unit = fabsf(scaled) >= 1.2e-38f ? scaled : 1.2e-38f;    // (not 0: an unseen place's infinite score stays one)
 
     // ---- loading: this lane's source offsets from the first of 16 places (pieces past head_dim: the place's first one again)
     uint32_t voff[S::kLoads];
@@ -83,7 +84,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
             const int place = lstep * kStep + 16 * a;
-            at[a] = (int64_t)args.layer * c.layer_stride + lp.head * c.head_stride + (page[a] < 0 ? 0 : page[a] * c.page_stride + (place & in_page) * c.place_stride);
+            at[a] = lp.head * c.head_stride + (page[a] < 0 ? 0 : page[a] * c.page_stride + (place & in_page) * c.place_stride);
         }
         no_pages = no_pages << 2 | (page[0] < 0 ? 1u : 0u) | (page[1] < 0 ? 2u : 0u);
 #pragma unroll
@@ -129,12 +130,15 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
             }
         }
     };
-    f32x4 o[NQ][kO];
-    float m[NQ], l[NQ];
+    // Rows' references: ref, minus the reference as the accumulators start from it, in units of raw scores (four times the same: an operand of the
+    // first product); the reference is 0 until the row's first score, and slack says so (kLowest, then kSlack)
+    f32x4 o[NQ][kO], ref[NQ];
+    float slack[NQ], l[NQ];
     auto clear = [&]() {
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
-            m[x] = kLowest;
+            ref[x] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            slack[x] = kLowest;
             l[x] = 0.f;
 #pragma unroll
             for (int j = 0; j < kO; ++j) o[x][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -153,7 +157,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
     load_q(p);
     clear();
     bool first_piece = true;
-    int step = p.step0;
+    int step = p.step0, masked_steps = 0;
+    if (threadIdx.x == 0) odd_in = 0;
     while (true) {
         wait_loads<S::kWait>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -163,6 +168,32 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
 
         const int p0 = step * kStep, end = p.len + p.tokens;
         const uint32_t no_page = no_pages >> 2 * (S::kBufs - 1) & 3;
+        const bool masked = p0 + kStep > p.len || no_page;
+        const uint32_t there = masked ? places_there(p0, end, no_page) : 0xffffffffu;
+        bool odd_values = false;
+        if (masked) {
+            // The block's wavefronts rid the stage's values of what must not meet even a weight of zero: places that are nobody's; and of new
+            // tokens, which some rows see and others do not, values that are no numbers or infinite, which are added below to the rows that see them.
+            ++masked_steps;
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < S::kLoads; ++i) {
+                const int n = wave * S::kLoads + i, place = n * S::kPlacesPerLoad + lane / S::kPieces;
+                const auto at = LDS_PTR(u32x4, buf + S::kHalf + n * 1024 + 16 * lane);
+                u32x4 v = *at;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t x = v[w];
+                    odd |= leave_out<F16>(x, there >> place & 1);
+                    v[w] = x;
+                }
+                *at = v;
+            }
+            if (__ballot(odd) && lane == 0) odd_in = masked_steps;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            odd_values = __builtin_amdgcn_readfirstlane(*(volatile int *)&odd_in) == masked_steps;
+        }
         f32x4 sc[NQ][2];
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
@@ -171,48 +202,78 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
             for (int k = 0; k < kKC; ++k)
                 if (EXACT || 32 * k < D) kf[k] = *LDS_PTR(u32x4, ((buf + ka) ^ (k << 6)) + 16 * a * S::kRow);
 #pragma unroll
-            for (int x = 0; x < NQ; ++x) sc[x][a] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int x = 0; x < NQ; ++x) sc[x][a] = ref[x];
 #pragma unroll
             for (int k = 0; k < kKC; ++k)
                 if (EXACT || 32 * k < D)
 #pragma unroll
                     for (int x = 0; x < NQ; ++x) sc[x][a] = mma<F16>(__builtin_bit_cast(uint4, kf[k]), qf[x][k], sc[x][a]);
         }
-        const bool masked = p0 + kStep > p.len || no_page;
-        uint32_t seen[NQ], there = 0xffffffffu;
+        uint32_t seen[NQ];
         if (masked) {
-            there = places_there(p0, end, no_page);
 #pragma unroll
             for (int x = 0; x < NQ; ++x) {
                 int t, h;
                 seen[x] = places_seen(call, p.first, row_of(p, x, t, h) ? t : 0, p0 - p.len, there);
+#pragma unroll
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(seen[x] >> (16 * a + 4 * g + i) & 1)) sc[x][a][i] = unit < 0.f ? -kNegInf : kNegInf;
+            }
+        }
+        // scores in bits, relative to the references; where one passes its reference by too much, or a row has its first, sums are scaled
+        float top[NQ];
+        bool moves = false;
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            sc[x][0] *= unit;
+            sc[x][1] *= unit;
+            top[x] = row_max(fmaxf(fmaxf(fmaxf(sc[x][0][0], sc[x][0][1]), fmaxf(sc[x][0][2], sc[x][0][3])),
+                                   fmaxf(fmaxf(sc[x][1][0], sc[x][1][1]), fmaxf(sc[x][1][2], sc[x][1][3]))));
+            moves |= top[x] > slack[x];
+        }
+        if (__ballot(moves)) {
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+                const bool first_one = slack[x] == kLowest;
+                const float by = top[x] > slack[x] ? top[x] : 0.f, f = first_one ? 0.f : __builtin_amdgcn_exp2f(-by);
+                if (top[x] > slack[x]) slack[x] = kSlack;
+                const float raw = ref[x][0] - by / unit;
+                ref[x] = (f32x4){raw, raw, raw, raw};
+                l[x] *= f;
+                sc[x][0] -= by;
+                sc[x][1] -= by;
+#pragma unroll
+                for (int j = 0; j < kO; ++j) o[x][j] *= f;
             }
         }
         uint4 pf[NQ];
-        weigh<F16, NQ, kO>(sc, masked, seen, g, unit, negative, m, l, o, pf);
-        bool odd_values = false;
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            float w[8];
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[4 * a + i] = __builtin_amdgcn_exp2f(sc[x][a][i]);
+            l[x] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            pf[x] = make_uint4(pack2<F16>(w[0], w[1]), pack2<F16>(w[2], w[3]), pack2<F16>(w[4], w[5]), pack2<F16>(w[6], w[7]));
+        }
 #pragma unroll
         for (int j = 0; j < kO; ++j) {
-            if (!EXACT && 16 * j >= D) continue;
             const uint32_t at = (buf + va) ^ (j << 5);
             const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at)));
             const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at + 16 * S::kRow)));
-            uint4 v = make_uint4(lo.x, lo.y, hi.x, hi.y);
-            if (masked) {
-                odd_values |= leave_out<F16>(v.x, there, 4 * g);
-                odd_values |= leave_out<F16>(v.y, there, 4 * g + 2);
-                odd_values |= leave_out<F16>(v.z, there, 16 + 4 * g);
-                odd_values |= leave_out<F16>(v.w, there, 16 + 4 * g + 2);
-            }
+            const uint4 v = make_uint4(lo.x, lo.y, hi.x, hi.y);
 #pragma unroll
             for (int x = 0; x < NQ; ++x) o[x][j] = mma<F16>(v, pf[x], o[x][j]);
         }
-        if (masked && __ballot(odd_values)) {
+        if (odd_values) {
             // rare: the values left out, place by place, to the rows that see the place (whatever its weight: the result is no number or infinite)
             for (int n = 0; n < 32; ++n) {
                 if (!(there >> n & 1)) continue;
                 const int place = p0 + n, of = page_of(c, p.slot, place);
-                const uint16_t *vr = c.v + (int64_t)args.layer * c.layer_stride + p.head * c.head_stride + of * c.page_stride + (place & in_page) * c.place_stride;
+                const uint16_t *vr = c.v + p.head * c.head_stride + of * c.page_stride + (place & in_page) * c.place_stride;
 #pragma unroll
                 for (int j = 0; j < kO; ++j)
 #pragma unroll
@@ -232,7 +293,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
 
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
-            const float sum = row_sum(l[x]);
+            const float sum = row_sum(l[x]), m = slack[x] == kLowest ? kLowest : -ref[x][0] * unit;
             int t, h;
             if (!row_of(p, x, t, h)) continue;
             if (p.whole) {
@@ -242,14 +303,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
                 for (int j = 0; j < kO; ++j)
                     if (EXACT || 16 * j + 4 * g < D)
                         *reinterpret_cast<uint2 *>(to + 16 * j) = make_uint2(pack2<F16>(o[x][j][0] * inv, o[x][j][1] * inv), pack2<F16>(o[x][j][2] * inv, o[x][j][3] * inv));
-                if (call.lse && g == 0) call.lse[(int64_t)(p.first + t) * call.q_heads + h] = lse_of(m[x], sum);
+                if (call.lse && g == 0) call.lse[(int64_t)(p.first + t) * call.q_heads + h] = lse_of(m, sum);
             } else {
                 float *piece = args.pieces + (size_t)(2 * run.block + (first_piece ? 0 : 1)) * piece_floats(kRows, DP);
                 const int row = (wave * NQ + x) * 16 + r;
 #pragma unroll
                 for (int j = 0; j < kO; ++j) *reinterpret_cast<f32x4 *>(piece + (size_t)row * DP + 16 * j + 4 * g) = o[x][j];
                 if (g == 0) {
-                    piece[(size_t)kRows * DP + row] = m[x];
+                    piece[(size_t)kRows * DP + row] = m;
                     piece[(size_t)kRows * (DP + 1) + row] = sum;
                 }
             }
