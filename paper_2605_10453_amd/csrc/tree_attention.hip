@@ -19,11 +19,14 @@
 namespace slimspec {
 namespace {
 
+constexpr int kWaves = 4, kThreads = 64 * kWaves;                      // of a block
+constexpr int kMergeWaves = 4, kMergeThreads = 64 * kMergeWaves;
+
 template <int NQ, int WR> struct TileOf { static constexpr int kRows = 16 * NQ * WR, kWT = kWaves / WR, kPlaces = kStep * kWT; };
 
 // DP: head_dim rounded up to 64, 128 or 256; EXACT: head_dim is DP
 template <bool F16, int DP, bool EXACT, int NQ, int WR>
-__global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_rows_kernel(TreeArgs args)
+__global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_rows_kernel(TreeArgs args)
 {
     const CacheView &c = args.c;
     const TreeCall &call = args.call;
@@ -37,7 +40,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
     const int group = call.q_heads / c.heads;
     Division div;
     __shared__ int4 near[kNear];
-    Run run = divide(c, b, group, tile, div, args.plan, near);
+    Run run = divide<kWaves>(c, b, group, tile, div, args.plan, near);
     if (run.u >= run.end) return;
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wt = wave / WR;
@@ -136,8 +139,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
             for (int j = 0; j < kO; ++j) o[x][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
         for (int step = p.step0; step < p.step1; ++step) {
+            // (the last step of a tile may have no places for this wavefront: none is `there` then)
             const int p0 = (step * kWT + wt) * kStep;
-            if (p0 >= end) break;                                      // (the last step of a tile may have no places for this wavefront)
             // V of this step: pieces of the eight places (tile a, 4 g + i) that the lane's weights are for
             uint32_t vf[8][kHalves * kVW / 2];
 #pragma unroll
@@ -170,14 +173,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
                     sc[x][a] = acc;
                 }
             __builtin_amdgcn_sched_barrier(0);
-            const bool masked = p0 + kStep > len || page[0] < 0 || page[1] < 0;
+            // the keys of what comes next, this piece's or the next one's, while this step's weights are made
+            const bool last = step + 1 == p.step1;
             const int page0 = page[0], page1 = page[1];
-            // the next step's keys while this one's weights are made
-            page[0] = next[0]; page[1] = next[1];
-            load_k(p, step + 1, page);
-            pages_of_step(p, step + 2, next);
+#pragma unroll
+            for (int a = 0; a < 2; ++a) page[a] = last ? (more ? soon[a] : -1) : next[a];
+            load_k(last ? q : p, last ? q.step0 : step + 1, page);
+            if (!last) pages_of_step(p, step + 2, next);
             __builtin_amdgcn_sched_barrier(0);
-
+            const bool masked = p0 + kStep > len || page0 < 0 || page1 < 0;
             uint32_t seen[NQ], there = 0xffffffffu;
             if (masked) {
                 there = places_there(p0, end, (page0 < 0 ? 1u : 0u) | (page1 < 0 ? 2u : 0u));
@@ -231,11 +235,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 2 : 3) void tree_ro
             }
         }
 
-        // the next piece's first loads, before this one's rows are joined and written
         if (more) {
 #pragma unroll
-            for (int a = 0; a < 2; ++a) { page[a] = soon[a]; next[a] = then[a]; }
-            load_k(q, q.step0, page);
+            for (int a = 0; a < 2; ++a) next[a] = then[a];
             load_q(q);
         }
         // the wavefronts of the same rows join: halves to halves, through shared memory in the accumulators' own layout
@@ -326,13 +328,13 @@ __device__ __forceinline__ const float *piece_at(const float *pieces, size_t str
 // a block per query row.  DP / 4 lanes hold a piece's row, so that the block goes over 1024 / DP pieces at a time; the partial sums meet across
 // lanes and in shared memory.
 template <bool F16, int DP>
-__global__ __launch_bounds__(kThreads) void tree_merge_rows_kernel(TreeArgs args, Tiling tile)
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_rows_kernel(TreeArgs args, Tiling tile)
 {
     const CacheView &c = args.c;
     const TreeCall &call = args.call;
     const BatchView &b = args.b;
     constexpr int kLanes = DP / 4, kPieces = kWave / kLanes;
-    __shared__ __align__(16) float joint[kWaves * (DP + 2)];
+    __shared__ __align__(16) float joint[kMergeWaves * (DP + 2)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = call.q_heads / c.heads;
     const int token = blockIdx.x / call.q_heads, qh = blockIdx.x - token * call.q_heads;
     Division div{args.plan->units, args.plan->blocks};
@@ -357,7 +359,7 @@ __global__ __launch_bounds__(kThreads) void tree_merge_rows_kernel(TreeArgs args
     const int d = 4 * (lane % kLanes);
     float m = kLowest, sum = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    constexpr int kAhead = 4, kApart = kPieces * kWaves;
+    constexpr int kAhead = 4, kApart = kPieces * kMergeWaves;
     for (int k0 = b0 + wave * kPieces + lane / kLanes; k0 <= b1; k0 += kAhead * kApart) {
         float mk[kAhead], lk[kAhead];
         f32x4 ok[kAhead];
@@ -398,12 +400,12 @@ __global__ __launch_bounds__(kThreads) void tree_merge_rows_kernel(TreeArgs args
     }
     if (lane < kLanes) {
         *reinterpret_cast<f32x4 *>(joint + wave * DP + d) = o;
-        if (lane == 0) { joint[kWaves * DP + wave] = m; joint[kWaves * (DP + 1) + wave] = sum; }
+        if (lane == 0) { joint[kMergeWaves * DP + wave] = m; joint[kMergeWaves * (DP + 1) + wave] = sum; }
     }
     __syncthreads();
     if (wave != 0 || lane >= kLanes) return;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) join(joint[kWaves * DP + w], joint[kWaves * (DP + 1) + w], *reinterpret_cast<const f32x4 *>(joint + w * DP + d));
+    for (int w = 1; w < kMergeWaves; ++w) join(joint[kMergeWaves * DP + w], joint[kMergeWaves * (DP + 1) + w], *reinterpret_cast<const f32x4 *>(joint + w * DP + d));
     const float inv = inverse(sum);
     if (d < c.head_dim)
         *reinterpret_cast<uint2 *>(call.out + (int64_t)token * call.out_token_stride + (int64_t)qh * call.out_head_stride + d) =
@@ -415,7 +417,7 @@ __global__ __launch_bounds__(kThreads) void tree_merge_rows_kernel(TreeArgs args
 // the blocks (k, *) join the tile, four lots of four channels to a thread.
 constexpr int kLots = 4;
 template <bool F16, int DP>
-__global__ __launch_bounds__(kThreads) void tree_merge_tiles_kernel(TreeArgs args, Tiling tile)
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_tiles_kernel(TreeArgs args, Tiling tile)
 {
     const CacheView &c = args.c;
     const TreeCall &call = args.call;
@@ -447,7 +449,7 @@ __global__ __launch_bounds__(kThreads) void tree_merge_tiles_kernel(TreeArgs arg
     f32x4 o[kLots];
 #pragma unroll
     for (int x = 0; x < kLots; ++x) {
-        const int e = (blockIdx.y * kLots + x) * kThreads + threadIdx.x;
+        const int e = (blockIdx.y * kLots + x) * kMergeThreads + threadIdx.x;
         in[x] = e / (DP / 4);
         d[x] = 4 * (e % (DP / 4));
         m[x] = kLowest;
@@ -499,7 +501,7 @@ Choice choose(int n, int tokens, int group, int head_dim)
     }
     k.nq = rows > 16 && dp != 256 ? 2 : 1;
     k.wr = rows <= 16 * k.nq ? 1 : rows <= 32 * k.nq ? 2 : 4;
-    k.blocks = 256 * (dp == 256 || k.nq > 1 ? 2 : 3);
+    k.blocks = 512;
     k.rows = 16 * k.nq * k.wr;
     k.places = kStep * kWaves / k.wr;
     return k;
@@ -510,10 +512,10 @@ hipError_t merge(const TreeArgs &a, const Choice &k, hipStream_t st)
 {
     const int64_t rows = (int64_t)a.b.tokens * a.call.q_heads;
     const Tiling tile{k.rows, k.places};
-    if (rows <= 2048) tree_merge_rows_kernel<F16, DP><<<(unsigned)rows, kThreads, 0, st>>>(a, tile);
+    if (rows <= 2048) tree_merge_rows_kernel<F16, DP><<<(unsigned)rows, kMergeThreads, 0, st>>>(a, tile);
     else {
-        const int lots = k.rows * (DP / 4), per_block = kLots * kThreads;
-        tree_merge_tiles_kernel<F16, DP><<<dim3(k.blocks - 1, (lots + per_block - 1) / per_block), kThreads, 0, st>>>(a, tile);
+        const int lots = k.rows * (DP / 4), per_block = kLots * kMergeThreads;
+        tree_merge_tiles_kernel<F16, DP><<<dim3(k.blocks - 1, (lots + per_block - 1) / per_block), kMergeThreads, 0, st>>>(a, tile);
     }
     return hipGetLastError();
 }

@@ -12,7 +12,6 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kWaves = 4;        // of a block
 constexpr int kStep = 32;                        // places per wavefront and step
 constexpr float kLowest = -3.0e38f;              // reference of a row without scores: finite, so that differences to it are numbers
 constexpr float kSlack = 8.f;                    // scores may pass the reference by this (in bits) before sums are scaled
@@ -121,13 +120,14 @@ constexpr int kNear = 256;                       // the first so many sequences 
 struct Run { int block; int64_t u, end; int seq; int64_t seq_start; Sequence s; };       // units [u, end) (none: u = end); the sequence of u and its first unit
 // A block's run.  Up to 64 sequences: every wavefront works it out by itself, a lane per sequence, without shared memory or a barrier; beyond,
 // the block's threads share the sequences.  Block 0 leaves the plan for the merge.
+template <int WAVES>
 __device__ __forceinline__ Run divide(const CacheView &c, const BatchView &b, int group, const Tiling &tile, Division &d, TreePlan *plan, int4 *near)
 {
-    __shared__ int64_t wave_sum[kWaves], found_start;
+    __shared__ int64_t wave_sum[WAVES], found_start;
     __shared__ int found;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const bool few = b.n <= kWave;
-    const int each = few ? 1 : (b.n + kThreads - 1) / kThreads, who = few ? lane : (int)threadIdx.x;
+    const int each = few ? 1 : (b.n + kWave * WAVES - 1) / (kWave * WAVES), who = few ? lane : (int)threadIdx.x;
     const int i0 = min(b.n, who * each), i1 = min(b.n, i0 + each);
     Sequence s = {};
     int64_t mine = 0;
@@ -147,7 +147,7 @@ __device__ __forceinline__ Run divide(const CacheView &c, const BatchView &b, in
         __syncthreads();
         total = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             if (w < wave) before += wave_sum[w];
             total += wave_sum[w];
         }

@@ -15,6 +15,8 @@
 namespace slimspec {
 namespace {
 
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #define LDS_PTR(T, byte_addr) ((__attribute__((address_space(3))) T *)(uintptr_t)(byte_addr))
@@ -50,7 +52,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
     const Tiling tile{kRows, kStep};
     const int group = call.q_heads / c.heads;
     Division div;
-    Run run = divide(c, b, group, tile, div, args.plan, near);
+    Run run = divide<kWaves>(c, b, group, tile, div, args.plan, near);
     if (run.u >= run.end) return;
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
