@@ -496,7 +496,7 @@ Choice choose(int n, int tokens, int group, int head_dim)
         k.nq = dp == 64 ? 4 : dp == 128 ? 3 : 1;
         k.blocks = 512;
         k.rows = 64 * k.nq;
-        k.places = kStep;
+        k.places = dp == 256 ? 32 : 64;
         return k;
     }
     k.nq = rows > 16 && dp != 256 ? 2 : 1;
