@@ -493,8 +493,10 @@ Choice choose(int n, int tokens, int group, int head_dim)
     Choice k{};
     k.tile = rows > 64;
     if (k.tile) {
-        k.nq = dp == 64 ? 4 : dp == 128 ? 3 : 1;
-        k.blocks = 512;
+        // as few rows of padding as possible
+        const int wide = dp == 64 ? 4 : 3;
+        k.nq = dp == 256 ? 1 : (rows + 127) / 128 * 2 <= (rows + 64 * wide - 1) / (64 * wide) * wide && dp == 128 ? 2 : wide;
+        k.blocks = dp == 64 && k.nq == 2 ? 768 : 512;
         k.rows = 64 * k.nq;
         k.places = dp == 256 ? 32 : 64;
         return k;

@@ -34,7 +34,7 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 template <int DP> struct Stage {
     static constexpr int kPlaces = DP == 256 ? 32 : 64, kSubs = kPlaces / kStep;
     static constexpr int kRow = 2 * DP, kHalf = kPlaces * kRow, kBytes = 2 * kHalf;    // a place; K; K and V
-    static constexpr int kBufs = DP == 64 ? 3 : 2;
+    static constexpr int kBufs = 2;
     static constexpr int kEach = kHalf / 1024 / kWaves, kLoads = 2 * kEach;            // loads per wavefront of each of K and V, of both
     static constexpr int kWait = (kBufs - 2) * kLoads;
     static constexpr int kPieces = DP / 8, kPlacesPerLoad = 64 / kPieces, kOwn = kPlaces / kWaves;      // (kOwn: places that a wavefront loads)
@@ -48,11 +48,12 @@ constexpr int kQueue = 8;                        // more than the pieces that kB
 struct Queue { Run run; Piece piece[kQueue]; };
 
 template <bool F16, int DP, bool EXACT, int NQ>
-__global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
+__global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_tile_kernel(TreeArgs args)
 {
     using S = Stage<DP>;
     static_assert(S::kBufs + 1 < kQueue, "the queue holds every piece that is loading or computed");
     constexpr int kKC = DP / 32, kO = DP / 16, kRows = 64 * NQ;
+    constexpr bool kEarly = !(DP == 128 && NQ == 3);                   // (there it takes more registers than there are)
     __shared__ __align__(1024) unsigned char stages[S::kBufs * S::kBytes];
     __shared__ int4 near[kNear];
     __shared__ Queue queues[kWaves];
@@ -133,6 +134,13 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
     const uint32_t ka = r * S::kRow + ((g ^ S::f(r)) << 4);
     const int vplace = 4 * g + (r >> 2);
     const uint32_t va = S::kHalf + vplace * S::kRow + ((((r >> 1) & 1) ^ S::f(vplace)) << 4) + ((r & 1) << 3);
+
+    auto read_v = [&](uint32_t at_sub, int j) {
+        const uint32_t at = (at_sub + va) ^ (j << 5);
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at)));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at + 16 * S::kRow)));
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    };
 
     // ---- this lane's query rows: number x in a piece is token t of the sequence and query head h
     uint4 qf[NQ][kKC];
@@ -243,7 +251,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
             const int p0 = stage0 + kStep * sub;
             if (sub > 0 && p0 >= end) break;
             const uint32_t at_sub = buf + sub * kStep * S::kRow;
-            uint4 pf[NQ];
+            uint4 pf[NQ], vf[kO];
             float sum[NQ];
             // Weights under the references as they are.  A lane's sum of eight beyond 2^8 says that a score may have passed its reference by
             // too much (always so where a row has none yet): then once more, with the references moved to the step's maxima, and the sums so far
@@ -263,6 +271,12 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
                         if (EXACT || 32 * k < D)
 #pragma unroll
                             for (int x = 0; x < NQ; ++x) sc[x][a] = mma<F16>(__builtin_bit_cast(uint4, kf[k]), qf[x][k], sc[x][a]);
+                }
+                // the values, on their way while the weights are made
+                if constexpr (kEarly) {
+#pragma unroll
+                    for (int j = 0; j < kO; ++j) vf[j] = read_v(at_sub, j);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
                 if (masked) {
 #pragma unroll
@@ -312,12 +326,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
             for (int x = 0; x < NQ; ++x) l[x] += sum[x];
 #pragma unroll
             for (int j = 0; j < kO; ++j) {
-                const uint32_t at = (at_sub + va) ^ (j << 5);
-                const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at)));
-                const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at + 16 * S::kRow)));
-                const uint4 v = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                if constexpr (!kEarly) vf[j] = read_v(at_sub, j);
 #pragma unroll
-                for (int x = 0; x < NQ; ++x) o[x][j] = mma<F16>(v, pf[x], o[x][j]);
+                for (int x = 0; x < NQ; ++x) o[x][j] = mma<F16>(vf[j], pf[x], o[x][j]);
             }
         }
         if (odd_values) {
@@ -383,9 +394,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(TreeArgs args)
 template <bool F16, int DP, bool EXACT>
 hipError_t launch_nq(const TreeArgs &a, int nq, int blocks, hipStream_t st)
 {
-    if constexpr (DP == 64) tree_tile_kernel<F16, DP, EXACT, 4><<<blocks, kThreads, 0, st>>>(a);
-    else if constexpr (DP == 128) tree_tile_kernel<F16, DP, EXACT, 3><<<blocks, kThreads, 0, st>>>(a);
-    else tree_tile_kernel<F16, DP, EXACT, 1><<<blocks, kThreads, 0, st>>>(a);
+    if constexpr (DP == 256) tree_tile_kernel<F16, DP, EXACT, 1><<<blocks, kThreads, 0, st>>>(a);
+    else if (nq == 2) tree_tile_kernel<F16, DP, EXACT, 2><<<blocks, kThreads, 0, st>>>(a);
+    else tree_tile_kernel<F16, DP, EXACT, DP == 64 ? 4 : 3><<<blocks, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 template <bool F16>
