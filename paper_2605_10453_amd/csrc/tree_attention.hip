@@ -24,7 +24,7 @@ constexpr int kMergeWaves = 4, kMergeThreads = 64 * kMergeWaves;
 
 template <int NQ, int WR> struct TileOf { static constexpr int kRows = 16 * NQ * WR, kWT = kWaves / WR, kPlaces = kStep * kWT; };
 
-// DP: head_dim rounded up to 64, 128 or 256; EXACT: head_dim is DP
+// DP: head_dim rounded up to 64 or 128 (more goes through tree_tile_kernel); EXACT: head_dim is DP
 template <bool F16, int DP, bool EXACT, int NQ, int WR>
 __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_rows_kernel(TreeArgs args)
 {
@@ -33,8 +33,8 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
     const BatchView &b = args.b;
     float *const pieces = args.pieces;
     using Tile = TileOf<NQ, WR>;
-    constexpr int kWT = Tile::kWT, kKC = DP / 32, kHalves = DP == 256 ? 2 : 1, kVW = DP == 64 ? 4 : 8;   // kVW: channels of V per lane and load
-    constexpr int kO = kHalves * kVW;                                                                    // accumulators (of 4) per row tile
+    constexpr int kWT = Tile::kWT, kKC = DP / 32, kVW = DP / 16;       // kVW: channels of V per lane and load
+    constexpr int kO = kVW;                                            // accumulators (of 4) per row tile
     __shared__ __align__(16) float joint[kWT > 1 ? (kWT / 2) * WR * (kO * NQ * 256 + 2 * NQ * 64) : 4];
     const Tiling tile{Tile::kRows, Tile::kPlaces};
     const int group = call.q_heads / c.heads;
@@ -51,14 +51,12 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
 
     // byte offsets of a lane's loads from the first of 16 places.  Channels past head_dim: the row's first piece again (for K, against
     // zeros of Q; what V gives there is not stored)
-    uint32_t koff[EXACT ? 1 : kKC], voff[4 * (EXACT ? 1 : kHalves)];
+    uint32_t koff[EXACT ? 1 : kKC], voff[4];
     const uint32_t row_bytes = 2 * (uint32_t)c.place_stride;
 #pragma unroll
     for (int k = 0; k < (EXACT ? 1 : kKC); ++k) koff[k] = r * row_bytes + (32 * k + 8 * g < D ? 2 * (32 * k + 8 * g) : 0);
 #pragma unroll
-    for (int h = 0; h < (EXACT ? 1 : kHalves); ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) voff[4 * h + i] = (4 * g + i) * row_bytes + (128 * h + kVW * r < D ? 2 * (128 * h + kVW * r) : 0);
+    for (int i = 0; i < 4; ++i) voff[i] = (4 * g + i) * row_bytes + (kVW * r < D ? 2 * kVW * r : 0);
 
     uint4 qf[NQ][kKC], kf[2][kKC];
     int page[2], next[2];
@@ -142,23 +140,20 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
             // (the last step of a tile may have no places for this wavefront: none is `there` then)
             const int p0 = (step * kWT + wt) * kStep;
             // V of this step: pieces of the eight places (tile a, 4 g + i) that the lane's weights are for
-            uint32_t vf[8][kHalves * kVW / 2];
+            uint32_t vf[8][kVW / 2];
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
                 const char *base = reinterpret_cast<const char *>(c.v + offset_of(p, step, a, page[a]));
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int h = 0; h < kHalves; ++h) {
-                        const char *from = base + voff[EXACT ? i : 4 * h + i] + (EXACT ? 256 * h : 0);
-                        if constexpr (kVW == 8) {
-                            const uint4 x = *reinterpret_cast<const uint4 *>(from);
-                            vf[4 * a + i][4 * h] = x.x; vf[4 * a + i][4 * h + 1] = x.y; vf[4 * a + i][4 * h + 2] = x.z; vf[4 * a + i][4 * h + 3] = x.w;
-                        } else {
-                            const uint2 x = *reinterpret_cast<const uint2 *>(from);
-                            vf[4 * a + i][0] = x.x; vf[4 * a + i][1] = x.y;
-                        }
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (kVW == 8) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(base + voff[i]);
+                        vf[4 * a + i][0] = x.x; vf[4 * a + i][1] = x.y; vf[4 * a + i][2] = x.z; vf[4 * a + i][3] = x.w;
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(base + voff[i]);
+                        vf[4 * a + i][0] = x.x; vf[4 * a + i][1] = x.y;
                     }
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
             f32x4 sc[NQ][2];
@@ -195,21 +190,19 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
 #pragma unroll
                 for (int n = 0; n < 8; ++n)
 #pragma unroll
-                    for (int w = 0; w < kHalves * kVW / 2; ++w) odd_values |= leave_out<F16>(vf[n][w], there >> (16 * (n >> 2) + 4 * g + (n & 3)) & 1);
+                    for (int w = 0; w < kVW / 2; ++w) odd_values |= leave_out<F16>(vf[n][w], there >> (16 * (n >> 2) + 4 * g + (n & 3)) & 1);
             }
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h)
 #pragma unroll
                 for (int j = 0; j < kVW; ++j) {
                     constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;       // (the second operand's halves are bytes 0 to 3)
-                    const int w = (kVW / 2) * h + (j >> 1);
+                    const int w = j >> 1;
                     uint4 a;
                     a.x = __builtin_amdgcn_perm(vf[1][w], vf[0][w], j & 1 ? kHigh : kLow);
                     a.y = __builtin_amdgcn_perm(vf[3][w], vf[2][w], j & 1 ? kHigh : kLow);
                     a.z = __builtin_amdgcn_perm(vf[5][w], vf[4][w], j & 1 ? kHigh : kLow);
                     a.w = __builtin_amdgcn_perm(vf[7][w], vf[6][w], j & 1 ? kHigh : kLow);
 #pragma unroll
-                    for (int x = 0; x < NQ; ++x) o[x][kVW * h + j] = mma<F16>(a, pf[x], o[x][kVW * h + j]);
+                    for (int x = 0; x < NQ; ++x) o[x][j] = mma<F16>(a, pf[x], o[x][j]);
                 }
             if (masked && __ballot(odd_values)) {
                 // rare: the values left out, place by place, to the rows that see the place (whatever its weight: the result is no number or infinite)
@@ -218,18 +211,16 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
                     const int a = n >> 4;
                     const uint16_t *vr = c.v + offset_of(p, step, a, a ? page1 : page0) + (n & 15) * c.place_stride;
 #pragma unroll
-                    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
                         for (int j = 0; j < kVW; ++j)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const int d = 128 * h + kVW * (4 * g + i) + j;
+                                const int d = kVW * (4 * g + i) + j;
                                 if (!EXACT && d >= D) continue;
                                 const uint16_t v = vr[d];
                                 if (!not_a_number_or_infinite<F16>(v)) continue;
 #pragma unroll
                                 for (int x = 0; x < NQ; ++x)
-                                    if (seen[x] >> n & 1) o[x][kVW * h + j][i] += value_of<F16>(v);
+                                    if (seen[x] >> n & 1) o[x][j][i] += value_of<F16>(v);
                             }
                 }
             }
@@ -279,14 +270,12 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
                     const float inv = inverse(sum);
                     uint16_t *to = call.out + (int64_t)(first + row_t[x]) * call.out_token_stride + (int64_t)row_h[x] * call.out_head_stride;
 #pragma unroll
-                    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
                         for (int e = 0; e < kVW / 2; ++e) {          // eight adjacent channels of the lane's 4 kVW
-                            const int d = 128 * h + 4 * kVW * g + 8 * e;
+                            const int d = 4 * kVW * g + 8 * e;
                             if (!EXACT && d >= D) continue;
                             float y[8];
 #pragma unroll
-                            for (int n = 0; n < 8; ++n) y[n] = o[x][kVW * h + (8 * e + n) % kVW][(8 * e + n) / kVW] * inv;
+                            for (int n = 0; n < 8; ++n) y[n] = o[x][(8 * e + n) % kVW][(8 * e + n) / kVW] * inv;
                             *reinterpret_cast<uint4 *>(to + d) = make_uint4(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]), pack2<F16>(y[4], y[5]), pack2<F16>(y[6], y[7]));
                         }
                     if (call.lse && g == 0)
@@ -295,13 +284,11 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
                     float *piece = pieces + (size_t)(2 * run.block + (first_piece ? 0 : 1)) * piece_floats(Tile::kRows, DP);
                     const int row = (wr * NQ + x) * 16 + r;
 #pragma unroll
-                    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
                         for (int e = 0; e < kVW; ++e) {              // four adjacent channels
-                            const int d = 128 * h + 4 * kVW * g + 4 * e;
+                            const int d = 4 * kVW * g + 4 * e;
                             f32x4 y;
 #pragma unroll
-                            for (int n = 0; n < 4; ++n) y[n] = o[x][kVW * h + (4 * e + n) % kVW][(4 * e + n) / kVW];
+                            for (int n = 0; n < 4; ++n) y[n] = o[x][(4 * e + n) % kVW][(4 * e + n) / kVW];
                             *reinterpret_cast<f32x4 *>(piece + (size_t)row * DP + d) = y;
                         }
                     if (g == 0) {
@@ -490,20 +477,21 @@ Choice choose(int n, int tokens, int group, int head_dim)
 {
     const int64_t rows = n > 0 ? (int64_t)((tokens + n - 1) / n) * group : 0;       // of an average sequence's key head
     const int dp = padded(head_dim);
+    const auto tiles_of = [&](int nq) { return (rows + 64 * nq - 1) / (64 * nq) * nq; };
     Choice k{};
-    k.tile = rows > 64;
+    k.blocks = 512;
+    k.tile = rows > (head_dim == 128 ? 32 : 64) || dp == 256;
     if (k.tile) {
-        // as few rows of padding as possible
-        const int wide = dp == 64 ? 4 : 3;
-        k.nq = dp == 256 ? 1 : (rows + 127) / 128 * 2 <= (rows + 64 * wide - 1) / (64 * wide) * wide && dp == 128 ? 2 : wide;
-        k.blocks = dp == 64 && k.nq == 2 ? 768 : 512;
+        if (dp == 256 || rows <= 64) k.nq = 1;
+        else if (dp == 128) k.nq = tiles_of(2) <= tiles_of(3) ? 2 : 3;
+        else k.nq = tiles_of(2) < tiles_of(4) ? 2 : 4;
+        if (dp == 64 && k.nq == 2) k.blocks = 768;
         k.rows = 64 * k.nq;
         k.places = dp == 256 ? 32 : 64;
         return k;
     }
-    k.nq = rows > 16 && dp != 256 ? 2 : 1;
-    k.wr = rows <= 16 * k.nq ? 1 : rows <= 32 * k.nq ? 2 : 4;
-    k.blocks = 512;
+    k.nq = rows > 16 ? 2 : 1;
+    k.wr = rows > 32 ? 2 : 1;
     k.rows = 16 * k.nq * k.wr;
     k.places = kStep * kWaves / k.wr;
     return k;
@@ -525,23 +513,18 @@ hipError_t merge(const TreeArgs &a, const Choice &k, hipStream_t st)
 template <bool F16, int DP, bool EXACT>
 hipError_t launch_rows(const TreeArgs &a, const Choice &k, hipStream_t st)
 {
-    if constexpr (DP == 256) {
-        if (k.wr == 1) tree_rows_kernel<F16, DP, EXACT, 1, 1><<<k.blocks, kThreads, 0, st>>>(a);
-        else if (k.wr == 2) tree_rows_kernel<F16, DP, EXACT, 1, 2><<<k.blocks, kThreads, 0, st>>>(a);
-        else tree_rows_kernel<F16, DP, EXACT, 1, 4><<<k.blocks, kThreads, 0, st>>>(a);
-    } else {
-        if (k.nq == 1) tree_rows_kernel<F16, DP, EXACT, 1, 1><<<k.blocks, kThreads, 0, st>>>(a);
-        else if (k.wr == 1) tree_rows_kernel<F16, DP, EXACT, 2, 1><<<k.blocks, kThreads, 0, st>>>(a);
-        else tree_rows_kernel<F16, DP, EXACT, 2, 2><<<k.blocks, kThreads, 0, st>>>(a);
-    }
+    if (k.nq == 1) tree_rows_kernel<F16, DP, EXACT, 1, 1><<<k.blocks, kThreads, 0, st>>>(a);
+    else if (k.wr == 1) tree_rows_kernel<F16, DP, EXACT, 2, 1><<<k.blocks, kThreads, 0, st>>>(a);
+    else if constexpr (!(DP == 128 && EXACT)) tree_rows_kernel<F16, DP, EXACT, 2, 2><<<k.blocks, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
 template <bool F16, int DP>
 hipError_t launch(const TreeArgs &a, const Choice &k, hipStream_t st)
 {
-    const hipError_t e = k.tile ? launch_tree_tile(a, k.nq, k.blocks, st)
-                       : a.c.head_dim == DP ? launch_rows<F16, DP, true>(a, k, st) : launch_rows<F16, DP, false>(a, k, st);
+    hipError_t e = hipSuccess;
+    if (k.tile) e = launch_tree_tile(a, k.nq, k.blocks, st);
+    else if constexpr (DP < 256) e = a.c.head_dim == DP ? launch_rows<F16, DP, true>(a, k, st) : launch_rows<F16, DP, false>(a, k, st);
     return e != hipSuccess ? e : merge<F16, DP>(a, k, st);
 }
 
@@ -557,17 +540,16 @@ hipError_t launch_type(const TreeArgs &a, const Choice &k, hipStream_t st)
 
 }  // namespace
 
-// The largest that a call of this many or fewer sequences and tokens can need: the widest tiling that so many rows take, all of one sequence.
+// The largest that a call of this many or fewer sequences and tokens can need: of the tilings that up to so many rows can take, the most.
 size_t tree_attention_workspace_bytes(int n, int tokens, int q_heads, int heads, int head_dim)
 {
-    const int group = q_heads / heads, dp = padded(head_dim);
-    size_t floats = 0;
-    for (const int64_t rows : {(int64_t)1, (int64_t)32, (int64_t)64, (int64_t)tokens * group}) {
-        const int t = (int)std::min<int64_t>(tokens, rows / group);
-        const Choice k = choose(1, t, group, head_dim);
-        floats = std::max(floats, 2 * (size_t)k.blocks * piece_floats(k.rows, dp));
-    }
-    return plan_bytes(n) + 4 * floats;
+    const int64_t rows = (int64_t)tokens * (q_heads / heads);
+    const int dp = padded(head_dim);
+    int64_t block_rows = 512 * (rows <= 16 ? 16 : rows <= 32 ? 32 : 64);
+    if (dp == 256) block_rows = 512 * 64;
+    else if (rows > 128) block_rows = 512 * (dp == 64 ? 256 : 192);
+    else if (rows > 64) block_rows = (dp == 64 ? 768 : 512) * 128;
+    return plan_bytes(n) + 4 * 2 * (size_t)block_rows * (dp + 2);
 }
 
 hipError_t launch_tree_attention(const CacheView &c, int layer, const TreeCall &call, const BatchView &b, void *workspace, hipStream_t st)

@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     using S = Stage<DP>;
     static_assert(S::kBufs + 1 < kQueue, "the queue holds every piece that is loading or computed");
     constexpr int kKC = DP / 32, kO = DP / 16, kRows = 64 * NQ;
-    constexpr bool kEarly = !(DP == 128 && NQ == 3);                   // (there it takes more registers than there are)
+    constexpr bool kEarly = !(DP == 128 && NQ == 3) && !(DP == 256 && !EXACT);     // (there it takes more registers than there are)
     __shared__ __align__(1024) unsigned char stages[S::kBufs * S::kBytes];
     __shared__ int4 near[kNear];
     __shared__ Queue queues[kWaves];
@@ -79,6 +79,9 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         stages_left = lane_value(run.end - run.u, 0);
         run_block = run.block;
         queue.run = run;                                               // (every lane the same)
+        // pieces past head_dim are never loaded: zeros, against zeros of Q
+        if constexpr (!EXACT)
+            for (int i = threadIdx.x; i < S::kBufs * S::kBytes / 16; i += kThreads) *LDS_PTR(u32x4, lds0 + 16 * i) = (u32x4){0u, 0u, 0u, 0u};
         if (threadIdx.x == 0) { odd_in = 0; page_missing[0] = page_missing[1] = 0; }
         __syncthreads();
     }
@@ -87,12 +90,14 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     const int in_page = (1 << c.page_shift) - 1;
     const float scaled = call.scale * kLog2e, unit = fabsf(scaled) >= 1.2e-38f ? scaled : 1.2e-38f;    // (not 0: an unseen place's infinite score stays one)
 
-    // ---- loading: this lane's source offsets from the first of 16 places (pieces past head_dim: the place's first one again)
+    // ---- loading: this lane's source offsets from the first of 16 places
     uint32_t voff[S::kEach];
+    bool loads[S::kEach];
 #pragma unroll
     for (int i = 0; i < S::kEach; ++i) {
         const int place = wave * S::kOwn + i * S::kPlacesPerLoad + lane / S::kPieces, piece = (lane % S::kPieces) ^ S::f(place);
-        voff[i] = (uint32_t)(place & 15) * 2u * (uint32_t)c.place_stride + (EXACT || 8 * piece < D ? 16u * piece : 0u);
+        voff[i] = (uint32_t)(place & 15) * 2u * (uint32_t)c.place_stride + 16u * piece;
+        loads[i] = EXACT || 8 * piece < D;
     }
     const int own_at = wave * S::kOwn & ~15;                           // of the stage's places, the first one of the 16 that this wavefront's lie in
     const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)c.table;
@@ -123,8 +128,10 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         const uint16_t *kp = c.k + from, *vp = c.v + from;
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
-            load_to_lds(buf + (wave * S::kEach + i) * 1024, voff[i], kp);
-            load_to_lds(buf + S::kHalf + (wave * S::kEach + i) * 1024, voff[i], vp);
+            if (loads[i]) {
+                load_to_lds(buf + (wave * S::kEach + i) * 1024, voff[i], kp);
+                load_to_lds(buf + S::kHalf + (wave * S::kEach + i) * 1024, voff[i], vp);
+            }
         }
         if (--stages_left > 0 && ++lstep == lstep1) load_next_piece();
         look_up();
@@ -246,8 +253,10 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             __builtin_amdgcn_s_barrier();
             odd_values = __builtin_amdgcn_readfirstlane(read_shared(&odd_in)) == masked_stages;
         }
+        // (a wavefront all of whose rows are past the sequence's tokens only loads)
+        const int subs = p.rt * kRows + wave * NQ * 16 < p.tokens * group ? S::kSubs : 0;
 #pragma unroll 1
-        for (int sub = 0; sub < S::kSubs; ++sub) {
+        for (int sub = 0; sub < subs; ++sub) {
             const int p0 = stage0 + kStep * sub;
             if (sub > 0 && p0 >= end) break;
             const uint32_t at_sub = buf + sub * kStep * S::kRow;
@@ -326,6 +335,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             for (int x = 0; x < NQ; ++x) l[x] += sum[x];
 #pragma unroll
             for (int j = 0; j < kO; ++j) {
+                if (!EXACT && j >= kO / 2 && 16 * j >= D) break;
                 if constexpr (!kEarly) vf[j] = read_v(at_sub, j);
 #pragma unroll
                 for (int x = 0; x < NQ; ++x) o[x][j] = mma<F16>(vf[j], pf[x], o[x][j]);
@@ -395,6 +405,7 @@ template <bool F16, int DP, bool EXACT>
 hipError_t launch_nq(const TreeArgs &a, int nq, int blocks, hipStream_t st)
 {
     if constexpr (DP == 256) tree_tile_kernel<F16, DP, EXACT, 1><<<blocks, kThreads, 0, st>>>(a);
+    else if (DP == 128 && EXACT && nq == 1) tree_tile_kernel<F16, 128, true, 1><<<blocks, kThreads, 0, st>>>(a);
     else if (nq == 2) tree_tile_kernel<F16, DP, EXACT, 2><<<blocks, kThreads, 0, st>>>(a);
     else tree_tile_kernel<F16, DP, EXACT, DP == 64 ? 4 : 3><<<blocks, kThreads, 0, st>>>(a);
     return hipGetLastError();
