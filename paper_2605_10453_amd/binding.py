@@ -538,9 +538,11 @@ _CACHE_DTYPES = {torch.bfloat16: SLIMSPEC_BF16, torch.float16: SLIMSPEC_F16}
 
 
 def _int32_ptr(t: torch.Tensor, name: str, shape: tuple) -> int:
-    if t.dtype != torch.int32 or tuple(t.shape) != shape:
+    if t.dtype is not torch.int32 or t.shape != shape:
         raise ValueError(f"{name} must be int32 {list(shape)}")
-    return _dev_ptr(t, name)
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    return t.data_ptr()
 
 
 def _empty(shape, dtype, device, stream):
@@ -576,6 +578,7 @@ class PagedCache:
         self.k, self.v, self.table, self.held, self.lens, self.refs = k, v, table, held, lens, refs
         self.layers, self.pages, self.heads, self.page_size, self.head_dim = layers, pages, heads, page_size, head_dim
         self.slots, self.slot_pages, self.dtype, self.device = slots, slot_pages, k.dtype, k.device
+        self._lib, self._row = load_library(), (heads, head_dim)
         self._struct = SlimspecCache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), k.stride(3),
                                      _int32_ptr(table, "table", (slots, slot_pages)), _int32_ptr(held, "held", (slots,)),
                                      _int32_ptr(lens, "lens", (slots,)), _int32_ptr(refs, "refs", (pages,)),
@@ -595,6 +598,13 @@ class PagedCache:
 def _batch(slots: torch.Tensor, first: torch.Tensor, tokens: int) -> SlimspecBatch:
     n = slots.shape[0]
     return SlimspecBatch(_int32_ptr(slots, "slots", (n,)), _int32_ptr(first, "first", (n + 1,)), n, tokens)
+
+
+def _cache_stream(cache: PagedCache, stream: Optional[torch.cuda.Stream]) -> int:
+    """The stream's handle; without one that of the current stream of the cache's device."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(cache.device.index)
+    return _stream_handle(stream)
 
 
 def _check(st: int) -> None:
@@ -620,35 +630,37 @@ def tree_attention(cache: PagedCache, layer: int, q: torch.Tensor, slots: torch.
     sequence's new ones, those of its row of mask (int64 [tokens, words], see `tree_mask`), or without a mask itself and the
     ones before it.  scale: head_dim ** -0.5 unless given.  lse [tokens, q_heads] float32, or False: not asked for.
     """
-    tokens, q_heads, head_dim = q.shape
-    if q.dtype != cache.dtype or head_dim != cache.head_dim or not q.is_cuda or q.stride(2) != 1:
+    shape = q.shape
+    tokens, q_heads, head_dim = shape
+    q_strides = q.stride()
+    if q.dtype is not cache.dtype or head_dim != cache.head_dim or not q.is_cuda or q_strides[2] != 1:
         raise ValueError("q must be a [tokens, q_heads, head_dim] device tensor of the cache's type and head_dim, its channels adjacent")
     if out is None:
         out = _empty((tokens, q_heads, head_dim), cache.dtype, cache.device, stream)
-    elif out.dtype != cache.dtype or out.shape != q.shape or not out.is_cuda or out.stride(2) != 1:
+    out_strides = out.stride()
+    if out.dtype is not cache.dtype or out.shape != shape or not out.is_cuda or out_strides[2] != 1:
         raise ValueError("out must be a device tensor of q's shape and type, its channels adjacent")
-    lse_ptr = None
     if lse is False:
-        lse = None
+        lse = lse_ptr = None
     else:
         if lse is None:
             lse = _empty((tokens, q_heads), torch.float32, cache.device, stream)
-        elif lse.dtype != torch.float32 or lse.shape != (tokens, q_heads):
+        elif lse.dtype is not torch.float32 or lse.shape != (tokens, q_heads):
             raise ValueError("lse must be float32 [tokens, q_heads]")
         lse_ptr = _dev_ptr(lse, "lse")
-    words, mask_ptr = 0, None
-    if mask is not None:
-        if mask.dtype != torch.int64 or mask.dim() != 2 or mask.shape[0] != tokens:
+    if mask is None:
+        words, mask_ptr = 0, None
+    else:
+        if mask.dtype is not torch.int64 or mask.dim() != 2 or mask.shape[0] != tokens:
             raise ValueError("mask must be int64 [tokens, words]")
         words, mask_ptr = mask.shape[1], _dev_ptr(mask, "mask")
-    lib = load_library()
+    lib = cache._lib
     batch = ctypes.byref(_batch(slots, first, tokens))
     if workspace is None:
         workspace = _empty((max(int(lib.slimspec_tree_attention_workspace_bytes(cache._ref, batch, q_heads)), 256),), torch.uint8, cache.device, stream)
-    qs, os_ = q.stride(), out.stride()
-    _check(lib.slimspec_tree_attention(cache._ref, layer, q.data_ptr(), q_heads, qs[0], qs[1], batch, mask_ptr, words,
-                                       head_dim ** -0.5 if scale is None else scale, out.data_ptr(), os_[0], os_[1], lse_ptr,
-                                       _dev_ptr(workspace, "workspace"), workspace.nbytes, _stream_handle(stream)))
+    _check(lib.slimspec_tree_attention(cache._ref, layer, q.data_ptr(), q_heads, q_strides[0], q_strides[1], batch, mask_ptr, words,
+                                       head_dim ** -0.5 if scale is None else scale, out.data_ptr(), out_strides[0], out_strides[1], lse_ptr,
+                                       _dev_ptr(workspace, "workspace"), workspace.nbytes, _cache_stream(cache, stream)))
     return out, lse
 
 
@@ -664,7 +676,8 @@ def tree_mask(parents: torch.Tensor, first: torch.Tensor, words: int, out: Optio
     elif out.dtype != torch.int64 or tuple(out.shape) != (tokens, words):
         raise ValueError("out must be int64 [tokens, words]")
     batch = SlimspecBatch(None, _int32_ptr(first, "first", (n + 1,)), n, tokens)
-    _check(load_library().slimspec_tree_mask(_int32_ptr(parents, "parents", (tokens,)), ctypes.byref(batch), words, _dev_ptr(out, "out"), _stream_handle(stream)))
+    handle = _raw_stream(parents.device.index) if stream is None and _raw_stream is not None and parents.is_cuda else _stream_handle(stream)
+    _check(load_library().slimspec_tree_mask(_int32_ptr(parents, "parents", (tokens,)), ctypes.byref(batch), words, _dev_ptr(out, "out"), handle))
     return out
 
 
@@ -675,25 +688,25 @@ def cache_reserve(cache: PagedCache, slots: torch.Tensor, first: torch.Tensor, r
         report = _empty((1,), torch.int32, cache.device, stream)
     # the number of tokens is not needed here: the ranges in `first` are taken as they are
     batch = _batch(slots, first, 0x7fffffff)
-    _check(load_library().slimspec_cache_reserve(cache._ref, ctypes.byref(batch), _int32_ptr(report, "report", (1,)), _stream_handle(stream)))
+    _check(cache._lib.slimspec_cache_reserve(cache._ref, ctypes.byref(batch), _int32_ptr(report, "report", (1,)), _cache_stream(cache, stream)))
     return report
 
 
 def cache_append(cache: PagedCache, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor, first: torch.Tensor,
                  stream: Optional[torch.cuda.Stream] = None) -> None:
     """Writes the new tokens' keys and values ([tokens, heads, head_dim], or [n_layers, tokens, heads, head_dim] from `layer` on) to their places."""
-    if k_new.shape != v_new.shape or k_new.stride() != v_new.stride() or k_new.dim() not in (3, 4):
+    shape, strides = k_new.shape, k_new.stride()
+    if shape != v_new.shape or strides != v_new.stride() or len(shape) not in (3, 4):
         raise ValueError("k_new and v_new must be [tokens, heads, head_dim] or [n_layers, tokens, heads, head_dim], with the same strides")
-    if k_new.dtype != cache.dtype or v_new.dtype != cache.dtype or not k_new.is_cuda or not v_new.is_cuda:
+    if k_new.dtype is not cache.dtype or v_new.dtype is not cache.dtype or not k_new.is_cuda or not v_new.is_cuda:
         raise ValueError("k_new and v_new must be device tensors of the cache's type")
-    shape, strides = tuple(k_new.shape), k_new.stride()
     if len(shape) == 3:
         shape, strides = (1, *shape), (0, *strides)
-    if shape[2:] != (cache.heads, cache.head_dim) or strides[3] != 1:
+    if shape[2:] != cache._row or strides[3] != 1:
         raise ValueError("k_new and v_new must have the cache's heads and head_dim, their channels adjacent")
     batch = _batch(slots, first, shape[1])
-    _check(load_library().slimspec_cache_append(cache._ref, layer, shape[0], k_new.data_ptr(), v_new.data_ptr(), *strides[:3],
-                                                ctypes.byref(batch), _stream_handle(stream)))
+    _check(cache._lib.slimspec_cache_append(cache._ref, layer, shape[0], k_new.data_ptr(), v_new.data_ptr(), *strides[:3],
+                                                ctypes.byref(batch), _cache_stream(cache, stream)))
 
 
 def cache_compact(cache: PagedCache, slots: torch.Tensor, first: torch.Tensor, path: torch.Tensor, accepted: torch.Tensor,
@@ -706,8 +719,8 @@ def cache_compact(cache: PagedCache, slots: torch.Tensor, first: torch.Tensor, p
         raise ValueError("path must be int32 [n, width]")
     width = path.shape[1]
     batch = _batch(slots, first, 0x7fffffff)
-    _check(load_library().slimspec_cache_compact(cache._ref, ctypes.byref(batch), _int32_ptr(path, "path", (n, width)), width,
-                                                 _int32_ptr(accepted, "accepted", (n,)), _int32_ptr(new_lens, "new_lens", (n,)), _stream_handle(stream)))
+    _check(cache._lib.slimspec_cache_compact(cache._ref, ctypes.byref(batch), _int32_ptr(path, "path", (n, width)), width,
+                                                 _int32_ptr(accepted, "accepted", (n,)), _int32_ptr(new_lens, "new_lens", (n,)), _cache_stream(cache, stream)))
     return new_lens
 
 
@@ -715,8 +728,8 @@ def cache_set_lens(cache: PagedCache, slots: torch.Tensor, lens: Optional[torch.
                    stream: Optional[torch.cuda.Stream] = None) -> None:
     """Sets the committed lengths of slots (None: 0, which frees them) and gives back the pages past them."""
     n = slots.shape[0]
-    _check(load_library().slimspec_cache_set_lens(cache._ref, _int32_ptr(slots, "slots", (n,)), n,
-                                                  None if lens is None else _int32_ptr(lens, "lens", (n,)), _stream_handle(stream)))
+    _check(cache._lib.slimspec_cache_set_lens(cache._ref, _int32_ptr(slots, "slots", (n,)), n,
+                                                  None if lens is None else _int32_ptr(lens, "lens", (n,)), _cache_stream(cache, stream)))
 
 
 def cache_fork(cache: PagedCache, parents: torch.Tensor, children: torch.Tensor, report: Optional[torch.Tensor] = None,
@@ -725,6 +738,6 @@ def cache_fork(cache: PagedCache, parents: torch.Tensor, children: torch.Tensor,
     n = parents.shape[0]
     if report is None:
         report = _empty((1,), torch.int32, cache.device, stream)
-    _check(load_library().slimspec_cache_fork(cache._ref, _int32_ptr(parents, "parents", (n,)), _int32_ptr(children, "children", (n,)), n,
-                                              _int32_ptr(report, "report", (1,)), _stream_handle(stream)))
+    _check(cache._lib.slimspec_cache_fork(cache._ref, _int32_ptr(parents, "parents", (n,)), _int32_ptr(children, "children", (n,)), n,
+                                              _int32_ptr(report, "report", (1,)), _cache_stream(cache, stream)))
     return report
