@@ -194,7 +194,9 @@ __device__ __forceinline__ Run divide(const CacheView &c, const BatchView &b, in
         __syncthreads();
         r.seq = __builtin_amdgcn_readfirstlane(found);
         r.seq_start = lane_value(found_start, 0);
-        r.s = sequence_of(c, b, r.seq);
+        const Sequence x = sequence_of(c, b, r.seq);
+        r.s = Sequence{__builtin_amdgcn_readfirstlane(x.slot), __builtin_amdgcn_readfirstlane(x.first), __builtin_amdgcn_readfirstlane(x.tokens),
+                       __builtin_amdgcn_readfirstlane(x.len), true};
     }
     return r;
 }
@@ -205,18 +207,20 @@ __device__ __forceinline__ Piece next_piece(const CacheView &c, const BatchView 
     int64_t units = units_of(c, r.s, group, tile);
     while (r.u >= r.seq_start + units) {
         r.seq_start += units;
-        if (++r.seq < kNear) {
-            const int4 x = near[r.seq];
-            r.s = Sequence{__builtin_amdgcn_readfirstlane(x.x), __builtin_amdgcn_readfirstlane(x.y), __builtin_amdgcn_readfirstlane(x.z), __builtin_amdgcn_readfirstlane(x.w), true};
-        } else
-            r.s = sequence_of(c, b, r.seq);
+        int4 x;
+        if (++r.seq < kNear) x = near[r.seq];
+        else {
+            const Sequence s = sequence_of(c, b, r.seq);
+            x = make_int4(s.slot, s.first, s.tokens, s.len);
+        }
+        r.s = Sequence{__builtin_amdgcn_readfirstlane(x.x), __builtin_amdgcn_readfirstlane(x.y), __builtin_amdgcn_readfirstlane(x.z), __builtin_amdgcn_readfirstlane(x.w), true};
         units = units_of(c, r.s, group, tile);
     }
     Piece p;
-    p.slot = __builtin_amdgcn_readfirstlane(r.s.slot);
-    p.len = __builtin_amdgcn_readfirstlane(r.s.len);
-    p.tokens = __builtin_amdgcn_readfirstlane(r.s.tokens);
-    p.first = __builtin_amdgcn_readfirstlane(r.s.first);
+    p.slot = r.s.slot;
+    p.len = r.s.len;
+    p.tokens = r.s.tokens;
+    p.first = r.s.first;
     const int steps = steps_of(r.s, tile), tiles = row_tiles(r.s, group, tile);
     const int64_t rel = r.u - r.seq_start;
     const int per_head = __builtin_amdgcn_readfirstlane(quotient(rel, steps));         // head * tiles + row tile

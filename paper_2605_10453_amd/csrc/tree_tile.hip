@@ -53,6 +53,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     using S = Stage<DP>;
     static_assert(S::kBufs + 1 < kQueue, "the queue holds every piece that is loading or computed");
     constexpr int kKC = DP / 32, kO = DP / 16, kRows = 64 * NQ;
+    constexpr bool kAhead = DP == 64 || (DP == 128 && NQ < 3);
     constexpr bool kEarly = !(DP == 128 && NQ == 3) && !(DP == 256 && !EXACT);     // (there it takes more registers than there are)
     __shared__ __align__(1024) unsigned char stages[S::kBufs * S::kBytes];
     __shared__ int4 near[kNear];
@@ -62,21 +63,24 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     // alike (two flags in turn): the wavefronts must agree on what they do between barriers.
     __shared__ int page_missing[2];
     const CacheView &c = args.c;
-    const TreeCall &call = args.call;
     const BatchView &b = args.b;
+    // Arguments that few stages need are read again there: kept in scalar registers through the loop they would push its own out.
+    const auto rare = []() __attribute__((always_inline)) {
+        auto *where = __builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(where));
+        return (const TreeArgs *)where;
+    };
     const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) unsigned char *)stages);
     const Tiling tile{kRows, S::kPlaces};
-    const int group = call.q_heads / c.heads;
+    const int group = __builtin_amdgcn_readfirstlane(args.call.q_heads / c.heads);
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Queue &queue = queues[wave];
-    int64_t stages_left;                                               // to load
     int run_block;
     {
         Division div;
         const Run run = divide<kWaves>(c, b, group, tile, div, args.plan, near);
         if (run.u >= run.end) return;
-        stages_left = lane_value(run.end - run.u, 0);
         run_block = run.block;
         queue.run = run;                                               // (every lane the same)
         // pieces past head_dim are never loaded: zeros, against zeros of Q
@@ -85,10 +89,9 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         if (threadIdx.x == 0) { odd_in = 0; page_missing[0] = page_missing[1] = 0; }
         __syncthreads();
     }
-    int64_t stages_to_do = stages_left;
     const int D = EXACT ? DP : c.head_dim;
     const int in_page = (1 << c.page_shift) - 1;
-    const float scaled = call.scale * kLog2e, unit = fabsf(scaled) >= 1.2e-38f ? scaled : 1.2e-38f;    // (not 0: an unseen place's infinite score stays one)
+    const float scaled = args.call.scale * kLog2e, unit = fabsf(scaled) >= 1.2e-38f ? scaled : 1.2e-38f;    // (not 0: an unseen place's infinite score stays one)
 
     // ---- loading: this lane's source offsets from the first of 16 places
     uint32_t voff[S::kEach];
@@ -100,12 +103,20 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         loads[i] = EXACT || 8 * piece < D;
     }
     const int own_at = wave * S::kOwn & ~15;                           // of the stage's places, the first one of the 16 that this wavefront's lie in
-    const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)c.table;
-    const auto *entries = table;                                       // of the slot that is loading
+    const int32_t *entries = c.table;                                  // of the slot that is loading
     int64_t head_at = 0;
-    int pushed = 0, popped = 0, turn = 0, lstep = 0, lstep1 = 0, lend = 0, entry = 0;
-    auto load_next_piece = [&]() {
-        Run run = queue.run;
+    int pushed = 0, popped = 0, turn = 0, lstep = 0, lstep1 = 0, lend = 0;
+    int entry = 0;                                                     // of the stage that is loaded next: looked up a stage ahead
+    auto load_next_piece = [&]() __attribute__((always_inline)) {
+        const Run &was = queue.run;                                    // (the same in every lane, which the compiler is told)
+        const auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        Run run{same(was.block), lane_value(was.u, 0), lane_value(was.end, 0), same(was.seq), lane_value(was.seq_start, 0),
+                Sequence{same(was.s.slot), same(was.s.first), same(was.s.tokens), same(was.s.len), true}};
+        if (run.u >= run.end) {                                        // nothing is left: what is loaded from here on is page 0, and nobody looks at it
+            lstep = lend = 0;
+            lstep1 = 0x7fffffff;
+            return;
+        }
         const Piece x = next_piece(c, b, group, tile, near, run);
         queue.run = run;
         queue.piece[pushed++ & (kQueue - 1)] = x;
@@ -113,28 +124,36 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         lstep1 = x.step1;
         lend = x.len + x.tokens;
         head_at = x.head * c.head_stride;
-        entries = table + (int64_t)x.slot * c.slot_pages;
+        entries = c.table + (int64_t)x.slot * c.slot_pages;
     };
-    // the page of the stage that is loaded next
-    auto look_up = [&]() {
+    // (A vector load, before the stage's own loads: it has arrived when they have.  A scalar one would be in flight with the reads of shared
+    // memory, which then wait for it: one counter for both, and scalar loads return out of order.)
+    auto look_up = [&]() __attribute__((always_inline)) {
         const int place = lstep * S::kPlaces + own_at;
-        entry = stages_left > 0 && place < lend ? entries[place >> c.page_shift] : 0;
+        int at = place < lend ? (place >> c.page_shift) * 4 : 0;       // (past the end: the slot's first entry, which is not used)
+        asm volatile("" : "+v"(at));
+        entry = *reinterpret_cast<const int32_t *>(reinterpret_cast<const char *>(entries) + at);
     };
-    auto issue = [&](uint32_t buf) {
-        const int place = lstep * S::kPlaces + own_at, page = __builtin_amdgcn_readfirstlane(entry);
-        const bool exists = (uint32_t)page < (uint32_t)c.pages;
-        if (!exists && lane == 0) page_missing[turn] = 1;
-        const int64_t from = head_at + (exists ? page * c.page_stride + (place & in_page) * c.place_stride : 0);
+    auto issue = [&](uint32_t buf) __attribute__((always_inline)) {
+        const int place = lstep * S::kPlaces + own_at;
+        int page = __builtin_amdgcn_readfirstlane(entry);
+        page = place < lend ? page : 0;
+        if (__builtin_expect((uint32_t)page >= (uint32_t)c.pages, 0)) {
+            if (lane == 0) page_missing[turn] = 1;
+            page = 0;
+        }
+        const int64_t from = head_at + (int64_t)((uint64_t)c.page_stride * (uint32_t)page + (uint32_t)c.place_stride * (uint32_t)(place & in_page));
+        const uint32_t to = buf + wave * S::kEach * 1024;
         const uint16_t *kp = c.k + from, *vp = c.v + from;
+        if (__builtin_expect(++lstep == lstep1, 0)) load_next_piece();
+        look_up();
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
             if (loads[i]) {
-                load_to_lds(buf + (wave * S::kEach + i) * 1024, voff[i], kp);
-                load_to_lds(buf + S::kHalf + (wave * S::kEach + i) * 1024, voff[i], vp);
+                load_to_lds(to + i * 1024, voff[i], kp);
+                load_to_lds(to + S::kHalf + i * 1024, voff[i], vp);
             }
         }
-        if (--stages_left > 0 && ++lstep == lstep1) load_next_piece();
-        look_up();
     };
 
     // ---- reading: K's fragment (a, k) at (buf + ka) ^ (k << 6), 16 a places on; V's (j, half) at (buf + va) ^ (j << 5), 16 places on
@@ -142,17 +161,24 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     const int vplace = 4 * g + (r >> 2);
     const uint32_t va = S::kHalf + vplace * S::kRow + ((((r >> 1) & 1) ^ S::f(vplace)) << 4) + ((r & 1) << 3);
 
-    auto read_v = [&](uint32_t at_sub, int j) {
+    auto read_v = [&](uint32_t at_sub, int j) __attribute__((always_inline)) {
         const uint32_t at = (at_sub + va) ^ (j << 5);
         const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at)));
         const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, at + 16 * S::kRow)));
         return make_uint4(lo.x, lo.y, hi.x, hi.y);
     };
 
+    uint4 kf[kAhead ? 2 : 1][kKC];
+    auto read_k = [&](uint32_t at_sub, int a) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < kKC; ++k)
+            if (EXACT || 32 * k < D) kf[kAhead ? a : 0][k] = __builtin_bit_cast(uint4, *LDS_PTR(u32x4, ((at_sub + ka) ^ (k << 6)) + 16 * a * S::kRow));
+    };
+
     // ---- this lane's query rows: number x in a piece is token t of the sequence and query head h
     uint4 qf[NQ][kKC];
     // (the divisor is hidden from the compiler: it would divide every stage for the few that need it)
-    auto row_of = [&](const Piece &p, int x, int &t, int &h) {
+    auto row_of = [&](const Piece &p, int x, int &t, int &h) __attribute__((always_inline)) {
         int by = group;
         asm volatile("" : "+s"(by));
         const int row = p.rt * kRows + (wave * NQ + x) * 16 + r;
@@ -162,7 +188,8 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     };
     f32x4 o[NQ][kO];
     float m[NQ], l[NQ];                                                // (the reference of a row without scores: kLowest)
-    auto begin_piece = [&](const Piece &p) {
+    auto begin_piece = [&](const Piece &p) __attribute__((always_inline)) {
+        const TreeCall call = rare()->call;
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             int t, h;
@@ -179,7 +206,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             for (int j = 0; j < kO; ++j) o[x][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
     };
-    auto pop = [&]() {
+    auto pop = [&]() __attribute__((always_inline)) {
         const Piece x = queue.piece[popped++ & (kQueue - 1)];
         Piece p;
         p.slot = __builtin_amdgcn_readfirstlane(x.slot);
@@ -197,7 +224,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     load_next_piece();
     look_up();
     uint32_t buf = lds0, buf_ahead = lds0;
-    auto next_buf = [&](uint32_t x) { return x + S::kBytes == lds0 + S::kBufs * S::kBytes ? lds0 : x + S::kBytes; };
+    auto next_buf = [&](uint32_t x) __attribute__((always_inline)) { return x + S::kBytes == lds0 + S::kBufs * S::kBytes ? lds0 : x + S::kBytes; };
 #pragma unroll
     for (int s = 0; s < S::kBufs - 1; ++s) {
         issue(buf_ahead);
@@ -255,6 +282,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         }
         // (a wavefront all of whose rows are past the sequence's tokens only loads)
         const int subs = p.rt * kRows + wave * NQ * 16 < p.tokens * group ? S::kSubs : 0;
+        if (kAhead && subs) { read_k(buf, 0); read_k(buf, 1); }
 #pragma unroll 1
         for (int sub = 0; sub < subs; ++sub) {
             const int p0 = stage0 + kStep * sub;
@@ -268,18 +296,25 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             while (true) {
                 f32x4 sc[NQ][2];
 #pragma unroll
-                for (int a = 0; a < 2; ++a) {
-                    u32x4 kf[kKC];
-#pragma unroll
-                    for (int k = 0; k < kKC; ++k)
-                        if (EXACT || 32 * k < D) kf[k] = *LDS_PTR(u32x4, ((at_sub + ka) ^ (k << 6)) + 16 * a * S::kRow);
-#pragma unroll
-                    for (int x = 0; x < NQ; ++x) sc[x][a] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                for (int x = 0; x < NQ; ++x) sc[x][0] = sc[x][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                if constexpr (kAhead) {
 #pragma unroll
                     for (int k = 0; k < kKC; ++k)
                         if (EXACT || 32 * k < D)
 #pragma unroll
-                            for (int x = 0; x < NQ; ++x) sc[x][a] = mma<F16>(__builtin_bit_cast(uint4, kf[k]), qf[x][k], sc[x][a]);
+                            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                                for (int x = 0; x < NQ; ++x) sc[x][a] = mma<F16>(kf[a][k], qf[x][k], sc[x][a]);
+                } else {
+#pragma unroll
+                    for (int a = 0; a < 2; ++a) {
+                        read_k(at_sub, a);
+#pragma unroll
+                        for (int k = 0; k < kKC; ++k)
+                            if (EXACT || 32 * k < D)
+#pragma unroll
+                                for (int x = 0; x < NQ; ++x) sc[x][a] = mma<F16>(kf[0][k], qf[x][k], sc[x][a]);
+                    }
                 }
                 // the values, on their way while the weights are made
                 if constexpr (kEarly) {
@@ -288,6 +323,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (masked) {
+                    const TreeCall call = rare()->call;
 #pragma unroll
                     for (int x = 0; x < NQ; ++x) {
                         int t, h;
@@ -333,6 +369,8 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             careful = false;
 #pragma unroll
             for (int x = 0; x < NQ; ++x) l[x] += sum[x];
+            // the next places' keys, on their way during the second product
+            if (kAhead && sub + 1 < subs) { read_k(at_sub + kStep * S::kRow, 0); read_k(at_sub + kStep * S::kRow, 1); }
 #pragma unroll
             for (int j = 0; j < kO; ++j) {
                 if (!EXACT && j >= kO / 2 && 16 * j >= D) break;
@@ -343,6 +381,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         }
         if (odd_values) {
             // rare: the values left out, place by place, to the rows that see the place (whatever its weight: the result is no number or infinite)
+            const TreeCall call = rare()->call;
             for (int n = 0; n < S::kPlaces; ++n) {
                 const int place = stage0 + n;
                 if (!((n < kStep ? there[0] : there[S::kSubs - 1]) >> (n & 31) & 1)) continue;
@@ -364,9 +403,10 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             }
         }
         buf = next_buf(buf);
-        --stages_to_do;
         if (++step < p.step1) continue;
 
+        const TreeCall call = rare()->call;
+        float *const pieces = rare()->pieces;
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             const float sum = row_sum(l[x]);
@@ -381,7 +421,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
                         *reinterpret_cast<uint2 *>(to + 16 * j) = make_uint2(pack2<F16>(o[x][j][0] * inv, o[x][j][1] * inv), pack2<F16>(o[x][j][2] * inv, o[x][j][3] * inv));
                 if (call.lse && g == 0) call.lse[(int64_t)(p.first + t) * call.q_heads + h] = lse_of(m[x], sum);
             } else {
-                float *piece = args.pieces + (size_t)(2 * run_block + (first_piece ? 0 : 1)) * piece_floats(kRows, DP);
+                float *piece = pieces + (size_t)(2 * run_block + (first_piece ? 0 : 1)) * piece_floats(kRows, DP);
                 const int row = (wave * NQ + x) * 16 + r;
 #pragma unroll
                 for (int j = 0; j < kO; ++j) *reinterpret_cast<f32x4 *>(piece + (size_t)row * DP + 16 * j + 4 * g) = o[x][j];
@@ -391,7 +431,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
                 }
             }
         }
-        if (stages_to_do == 0) break;
+        if (popped == pushed) break;                                   // (the loading side is a stage ahead: it has said what comes next)
         first_piece = false;
         p = pop();
         step = p.step0;
