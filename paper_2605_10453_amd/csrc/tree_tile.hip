@@ -295,6 +295,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             // scaled.  Looking for the maxima every time would be a sixth of the step's vector instructions.
             while (true) {
                 f32x4 sc[NQ][2];
+                if (DP == 64) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int x = 0; x < NQ; ++x) sc[x][0] = sc[x][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
                 if constexpr (kAhead) {
@@ -316,6 +317,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
                                 for (int x = 0; x < NQ; ++x) sc[x][a] = mma<F16>(kf[0][k], qf[x][k], sc[x][a]);
                     }
                 }
+                if (DP == 64) __builtin_amdgcn_s_setprio(0);
                 // the values, on their way while the weights are made
                 if constexpr (kEarly) {
 #pragma unroll
@@ -369,6 +371,10 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
             careful = false;
 #pragma unroll
             for (int x = 0; x < NQ; ++x) l[x] += sum[x];
+            // A wavefront at a product goes before one at its weights on the same SIMD: the matrix cores then start while the other's vector
+            // instructions fill in.  Longer heads keep it to the end of the stage (uniform contexts of 6000, 64 positions, 64 query heads: head_dim
+            // 64 158 -> 145 us, 151 if kept; 128 262 -> 246, 257 if given back before the weights).
+            __builtin_amdgcn_s_setprio(1);
             // the next places' keys, on their way during the second product
             if (kAhead && sub + 1 < subs) { read_k(at_sub + kStep * S::kRow, 0); read_k(at_sub + kStep * S::kRow, 1); }
 #pragma unroll
@@ -379,6 +385,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
                 for (int x = 0; x < NQ; ++x) o[x][j] = mma<F16>(vf[j], pf[x], o[x][j]);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         if (odd_values) {
             // rare: the values left out, place by place, to the rows that see the place (whatever its weight: the result is no number or infinite)
             const TreeCall call = rare()->call;
