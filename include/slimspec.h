@@ -277,7 +277,8 @@ int routed_head_topk_prepared(const void *h, const void *A, const void *B, const
  *
  * Supported: BF16 and F16; head_dim a multiple of 8 up to SLIMSPEC_CACHE_MAX_HEAD_DIM; page_size a
  * power of two, 16 to 1024; up to SLIMSPEC_CACHE_MAX_SEQUENCES sequences a call; slot_pages *
- * page_size < 2^31; place_stride <= 2^20.  Element offsets are 64 bits throughout. */
+ * page_size < 2^31; place_stride <= 2^20; up to 1024 layers and heads; tokens * q_heads < 2^31.  Element
+ * offsets are 64 bits throughout. */
 #define SLIMSPEC_CACHE_MAX_HEAD_DIM 256
 #define SLIMSPEC_CACHE_MAX_SEQUENCES 4096
 #define SLIMSPEC_TREE_MAX_WORDS 64

@@ -49,7 +49,7 @@ size_t slimspec_tree_attention_workspace_bytes(const slimspec_cache *cache, cons
 {
     CacheView c;
     if (check_cache(cache, c) != SLIMSPEC_OK || !batch || batch->n < 0 || batch->tokens < 0 || batch->n > SLIMSPEC_CACHE_MAX_SEQUENCES) return 0;
-    if (q_heads < 1 || q_heads % c.heads || q_heads > 65535) return 0;
+    if (q_heads < 1 || q_heads % c.heads || q_heads > 65535 || (int64_t)batch->tokens * q_heads >= (int64_t)1 << 31) return 0;
     return tree_attention_workspace_bytes(batch->n, batch->tokens, q_heads, c.heads, c.head_dim);
 }
 
@@ -68,7 +68,7 @@ int slimspec_tree_attention(const slimspec_cache *cache, int32_t layer,
     if (q_heads < 1 || q_heads % c.heads || !(scale - scale == 0.f)) return SLIMSPEC_INVALID_ARGUMENT;      // (a scale that is a finite number)
     if (mask && (mask_words < 1 || mask_words > SLIMSPEC_TREE_MAX_WORDS)) return SLIMSPEC_INVALID_ARGUMENT;
     if (q_token_stride < 0 || q_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0) return SLIMSPEC_INVALID_ARGUMENT;
-    if (q_heads > 65535) return SLIMSPEC_UNSUPPORTED;
+    if (q_heads > 65535 || (int64_t)b.tokens * q_heads >= (int64_t)1 << 31) return SLIMSPEC_UNSUPPORTED;       // query rows are counted in 31 bits
     if (!rows_aligned(q_token_stride) || !rows_aligned(q_head_stride) || !rows_aligned(out_token_stride) || !rows_aligned(out_head_stride)) return SLIMSPEC_UNSUPPORTED;
     if (b.n == 0 || b.tokens == 0) return SLIMSPEC_OK;
     if (!q || !out || !workspace) return SLIMSPEC_INVALID_ARGUMENT;

@@ -153,7 +153,11 @@ __device__ __forceinline__ Run divide(const CacheView &c, const BatchView &b, in
         }
     }
     d.units = total;
-    d.blocks = (int)(total < (int64_t)gridDim.x ? (total > 0 ? total : 1) : gridDim.x);
+    // runs of at least 128 places: shorter ones take longer to join than they save (one request of 64 positions at 3000 in runs of 64 places
+    // 32.2 us, of 128 26.6, 256 27.0; one token at 2000 in runs of 128 10.9, 256 11.5)
+    const int least = tile.places < 128 ? 128 / tile.places : 1;
+    const int64_t runs = (total + least - 1) / least;
+    d.blocks = (int)(runs < (int64_t)gridDim.x ? (runs > 0 ? runs : 1) : gridDim.x);
     if (blockIdx.x == 0 && (!few || wave == 0)) {
         if (threadIdx.x == 0) { plan->units = total; plan->blocks = d.blocks; }
         int64_t at = before;

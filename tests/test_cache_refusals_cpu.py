@@ -71,6 +71,7 @@ def test_attention_arguments(b):
         assert call(**bad) == b.STATUS_INVALID_ARGUMENT, bad
     for bad in (dict(q=FAKE + 2), dict(out=FAKE + 8), dict(qt=516), dict(qh=132), dict(ot=4), dict(oh=129), dict(ws=FAKE + 16), dict(heads=65536)):
         assert call(**bad) == b.STATUS_UNSUPPORTED, bad
+    assert call(x=batch(b, tokens=1 << 29)) == b.STATUS_UNSUPPORTED and lib.slimspec_tree_attention_workspace_bytes(cache(b), batch(b, tokens=1 << 29), 4) == 0
     need = lib.slimspec_tree_attention_workspace_bytes(cache(b), batch(b), 4)
     assert need > 0 and need % 256 == 0
     assert call(wsb=need - 1) == b.STATUS_WORKSPACE_TOO_SMALL
