@@ -5,6 +5,9 @@
 // depend on which block gave its pages back first.  Giving back and sharing are commutative integer atomics on refs; taking is one
 // block that scans refs from page 0 on, so the pages taken are the lowest free ones whatever ran before, and a call's outcome is a
 // function of the books alone.
+//
+// The books' kernels are a few loads one after the other (set_lens 1.3 us, reserve and the first launch of a fork 5 us, 8 to 9 for a batch of 64 to
+// 96: the scan of refs); the rows' kernels are bound by memory once there is enough to move (the figures are at each).
 #include "cache.hpp"
 
 namespace slimspec {
@@ -206,7 +209,8 @@ __global__ __launch_bounds__(kBookThreads) void cache_fork_books_kernel(CacheVie
 }
 
 // Fork, second launch: block (pair, layer) copies the rows of the page that is not full; the blocks of layer 0 share the full pages.
-// (What the parent's books say is read from the child, which has them since the first launch.)
+// (What the parent's books say is read from the child, which has them since the first launch.)  96 children of 24 parents, 32 layers of 4 heads of
+// 128, 31 rows on average: 65 us for 250 MB (four pieces in flight per thread instead of one: 92 us).
 __global__ __launch_bounds__(256) void cache_fork_rows_kernel(CacheView c, const int32_t *__restrict__ parents, const int32_t *__restrict__ children,
                                                               const int32_t *__restrict__ report)
 {
@@ -235,7 +239,8 @@ __global__ __launch_bounds__(256) void cache_fork_rows_kernel(CacheView c, const
     }
 }
 
-// Block (token, layer): the row's keys and values to the token's place.
+// Block (token, layer): the row's keys and values to the token's place.  22943 tokens of 8 heads of 128, one layer, 31 us (6.0 TB/s in and
+// out); 512 tokens 2.9 us, of which the loads that find the place are most.
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, int first_layer, NewRows rows, BatchView b)
 {
     __shared__ int found;
@@ -265,7 +270,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, int firs
 
 // Block (sequence, 256 columns of 16 bytes over layers, K and V, heads): a thread moves its column of all the path's rows, first to
 // last.  A row's place is never behind its source and the sources increase, so no row is overwritten before it has been read, with any
-// number of rows in flight; different threads' columns do not meet.
+// number of rows in flight; different threads' columns do not meet.  64 sequences, 32 layers, two or three rows each: 11.5 us.
 constexpr int kPathBatch = 64, kMoveBatch = 8;
 __global__ __launch_bounds__(256) void cache_compact_kernel(CacheView c, BatchView b, const int32_t *__restrict__ path, int width,
                                                             const int32_t *__restrict__ accepted, int32_t *__restrict__ new_lens)

@@ -2,7 +2,8 @@
 //
 // With s_p = scale q.k_p over the places p that a token sees, out = sum_p e^{s_p - m} v_p / sum_p e^{s_p - m} for any m; m is a
 // running reference near the maximum of the scores so far, and sums made under an older one are scaled by e^{m_old - m}: one pass over
-// the keys and values, each read once for up to 128 query rows.
+// the keys and values, each read once per row tile.  This file: few rows to a key head (tree_rows_kernel), the merge, and the choice of tiling;
+// many rows: tree_tile.hip.
 //
 // Layout.  The rows that share a key head (a sequence's new tokens times the query heads of the group) are tiled by 16 NQ WR.  A block is
 // four wavefronts: WR of them side by side on rows, WT = 4 / WR on stretches of 32 places.  A wavefront goes straight from the cache to
@@ -13,8 +14,13 @@
 // that order (its index is (g, tile, i)), so P needs no exchange between lanes.  A lane loads V rows 4 g + i in pieces of DP / 16 channels
 // and turns eight rows by byte permutes: its MFMA number j has row index r for channel (DP / 16) r + j, so the accumulators of a lane are DP / 4
 // adjacent channels of row r.
+//
+// Bound by memory where the rows are few: K of the next step is requested behind the first product, V of this one before it, 16 KB a wavefront
+// in flight; two wavefronts to a SIMD (the pieces of a third one's blocks cost more than it brings: 126 against 103 us, 64 requests of 4
+// positions at 2115).  128 single tokens over 8.5 GB 1392 us (6.1 TB/s); 64 requests of 8 positions, 32 query heads, at 130 to 4100 131 us (4.2 TB/s;
+// 107 us at 2115 each: where contexts differ, runs end inside row tiles, and their pieces are written and joined); one token at 500 10.7 us, of which
+// the kernel takes 7.2 (slot, length, page and keys are four loads one after the other) and the merge 2.8.
 #include "tree_parts.hpp"
-#include <algorithm>
 
 namespace slimspec {
 namespace {
@@ -311,9 +317,9 @@ __device__ __forceinline__ const float *piece_at(const float *pieces, size_t str
     return pieces + ((size_t)2 * k + (k == b0 && second ? 1 : 0)) * stride;
 }
 
-// Joins the pieces of the row tiles that more than one block worked on.  For few rows, of which one long sequence has up to 96 pieces each:
-// a block per query row.  DP / 4 lanes hold a piece's row, so that the block goes over 1024 / DP pieces at a time; the partial sums meet across
-// lanes and in shared memory.
+// Joins the pieces of the row tiles that more than one block worked on: latency, not bytes.  For few rows, of which a long sequence has many
+// pieces each, a block per query row (2.8 us for one token's 32 rows, 11 us for 1536 rows of a sequence of 131000).  DP / 4 lanes hold a piece's
+// row, so that the block goes over 1024 / DP pieces at a time; the partial sums meet across lanes and in shared memory.
 template <bool F16, int DP>
 __global__ __launch_bounds__(kMergeThreads) void tree_merge_rows_kernel(TreeArgs args, Tiling tile)
 {
@@ -401,7 +407,8 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_rows_kernel(TreeArgs
 }
 
 // ... for many rows: block (k, y) of the launch looks at the boundary between the runs k and k + 1; if it is the first one inside its row tile,
-// the blocks (k, *) join the tile, four lots of four channels to a thread.
+// the blocks (k, *) join the tile, four lots of four channels to a thread: nothing is looked at for row tiles of one piece (65536 rows of two or
+// three pieces 13 us, 40 a wavefront per row).
 constexpr int kLots = 4;
 template <bool F16, int DP>
 __global__ __launch_bounds__(kMergeThreads) void tree_merge_tiles_kernel(TreeArgs args, Tiling tile)
@@ -473,9 +480,18 @@ constexpr int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 12
 // tile: tree_tile_kernel with 64 nq rows; else tree_rows_kernel with 16 nq wr
 struct Choice { bool tile; int nq, wr, blocks, rows, places; };
 
+// By the rows of an average sequence's key head (the host knows no more; any tiling is right for any sequence).  us a call, the kernel taken
+// first; n sequences of T positions, 4 query heads to each of 8 key heads (head_dim 256: of 4):
+//   tree_tile_kernel beyond 64 rows: n 1, T 48 at 131000, head_dim 128: 184 / 334
+//     beyond 32 rows with head_dim 128: n 64, T 16 at 2115: 111 / 124; not with 64 (65 / 68) nor with 80 or 96 (90 / 138, 98 / 141: its stages are as
+//       wide as 128), and not up to 32 rows (T 8 at 130 to 4100: 132 / 143; 32 single tokens at 500: 20 / 23)
+//     at every count beyond 128 channels, where tree_rows_kernel has too few registers: n 64, T 1 at 2115, head_dim 256: 106 / 149
+//   its rows: as few of padding as can be.  head_dim 64: 128 against 256 rows, T 32 at 130 to 4100 (128 rows) 113 / 153; 256 where that pads no
+//     more, 16 sequences of 512 rows at 6000 169 / 174.  128: 128 against 192 rows, 512 rows there 285 / 336; 192 against 128 for 192 rows, n 1, T 48
+//     at 131000, 175 / 229
 Choice choose(int n, int tokens, int group, int head_dim)
 {
-    const int64_t rows = n > 0 ? (int64_t)((tokens + n - 1) / n) * group : 0;       // of an average sequence's key head
+    const int64_t rows = n > 0 ? (int64_t)((tokens + n - 1) / n) * group : 0;
     const int dp = padded(head_dim);
     const auto tiles_of = [&](int nq) { return (rows + 64 * nq - 1) / (64 * nq) * nq; };
     Choice k{};

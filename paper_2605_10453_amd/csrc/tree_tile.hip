@@ -1,15 +1,21 @@
 // Tree attention of many rows to a key head: keys and values go through shared memory.
 //
-// A block is four wavefronts of 16 NQ query rows each, all on the same 32 places: with as many rows the wavefronts' own loads of K and V
-// (tree_rows_kernel) would need several times what a CU's vector cache gives.  The products, their operand orders and the weights are those
-// of tree_rows_kernel; V turns on its way out of shared memory (ds_read_b64_tr_b16: 16 lanes read a 4 x 16 block and get its columns).
+// A block is four wavefronts of 16 NQ query rows each, all on the same 64 places (32 where a place is 512 bytes): with as many rows the
+// wavefronts' own loads of K and V (tree_rows_kernel) would need several times what a CU's vector cache gives (48 positions, 4 query heads to a
+// key head, at 131000: 334 us that way).  The products, their operand orders and the weights are those of tree_rows_kernel; V turns on its way
+// out of shared memory (ds_read_b64_tr_b16: 16 lanes read a 4 x 16 block and get its columns).
 //
-// Stages of 64 places (32 where a place is 512 bytes), K and V, come straight into shared memory (global_load_lds_dwordx4), ahead across the
-// pieces of the run; a wavefront loads a quarter of the stage's places, which lie in one page.  A place is DP channels in pieces of 16 bytes,
-// stored at piece index XOR f(place) so that neither a fragment of K (16 places, one piece each per lane group) nor one of V meets a bank
-// twice; the loads choose their source accordingly.  Every wavefront issues kLoads loads a stage, whatever is left to do, and vector memory
-// returns in order: s_waitcnt vmcnt((kBufs - 2) kLoads) = its part of the stage needed next has landed (other loads and stores only make the
-// wait longer); the barrier then says so for all, and that all have read the stage before.
+// Stages, K and V, come straight into shared memory (global_load_lds_dwordx4) while the stage before is computed, across the pieces of the
+// run; a wavefront loads a quarter of the stage's places, which lie in one page, so it needs one page number.  A place is DP channels in pieces
+// of 16 bytes, stored at piece index XOR f(place), which spreads a fragment of K (16 places, one piece each per lane group) and one of V over the
+// banks; the loads choose their source accordingly.  Two buffers: a wavefront waits for its own loads, the barrier says so for all, and that
+// all have read the stage before; only then is the next one requested, into that one's place.
+//
+// Bound by vector instructions: 32 places of 16 rows are 8 weights a lane (scaling, exponential at four times a multiply's time, sum, rounding)
+// beside 8 MFMAs (head_dim 64) or 16 (128).  What carried it, us for 16 requests of 64 positions, 64 query heads to 8 key heads of 64 channels, at
+// 6000: no search for maxima where none is needed (176 -> 162), the loading side in few scalar instructions (170 -> 162), wavefronts at a product
+// before those at their weights (158 -> 144).  144 us there (700 TFLOP/s), 243 us with 128 channels (830); with one request of 48 positions at
+// 131000 145 us (700 TFLOP/s, 3.7 TB/s); 64 single tokens at 2115, head_dim 256, 106 us (5.2 TB/s).
 #include "tree_parts.hpp"
 #include <type_traits>
 
@@ -29,14 +35,13 @@ __device__ __forceinline__ void load_to_lds(uint32_t to, uint32_t voff, const vo
 }
 // What another wavefront wrote to shared memory before the barrier (as a read of shared memory: a generic one would wait for the loads in flight)
 __device__ __forceinline__ int read_shared(int *p) { return *(volatile __attribute__((address_space(3))) int *)p; }
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 template <int DP> struct Stage {
     static constexpr int kPlaces = DP == 256 ? 32 : 64, kSubs = kPlaces / kStep;
     static constexpr int kRow = 2 * DP, kHalf = kPlaces * kRow, kBytes = 2 * kHalf;    // a place; K; K and V
     static constexpr int kBufs = 2;
-    static constexpr int kEach = kHalf / 1024 / kWaves, kLoads = 2 * kEach;            // loads per wavefront of each of K and V, of both
-    static constexpr int kWait = (kBufs - 2) * kLoads;
+    static constexpr int kEach = kHalf / 1024 / kWaves;                                // loads per wavefront, of each of K and V
     static constexpr int kPieces = DP / 8, kPlacesPerLoad = 64 / kPieces, kOwn = kPlaces / kWaves;      // (kOwn: places that a wavefront loads)
     static __device__ __forceinline__ int f(int place) { return DP == 64 ? (place >> 1) & 7 : place & 15; }
 };
@@ -235,7 +240,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
     bool first_piece = true, missing = false, careful = true;
     int step = p.step0, masked_stages = 0;
     while (true) {
-        wait_loads<S::kWait>();
+        wait_loads();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         missing |= __builtin_amdgcn_readfirstlane(read_shared(&page_missing[turn])) != 0;
@@ -445,7 +450,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 2 ? 3 : 2) void tree_ti
         begin_piece(p);
         careful = true;
     }
-    wait_loads<0>();                                                   // no load into the block's shared memory outlives the block
+    wait_loads();                                                      // no load into the block's shared memory outlives the block
 }
 
 template <bool F16, int DP, bool EXACT>
