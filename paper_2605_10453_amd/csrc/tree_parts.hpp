@@ -14,7 +14,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 32;                        // places per wavefront and step
 constexpr float kLowest = -3.0e38f;              // reference of a row without scores: finite, so that differences to it are numbers
-constexpr float kSlack = 8.f;                    // scores may pass the reference by this (in bits) before sums are scaled
+constexpr float kSlack = 8.f;                    // scores may pass the reference by this (in bits) before sums are scaled: weights up to 2^8 round as well as weights up to 1, and f16 holds them
 
 template <bool F16>
 __device__ __forceinline__ f32x4 mma(uint4 a, uint4 b, f32x4 c)
@@ -62,7 +62,7 @@ __device__ __forceinline__ float row_sum(float v)
 //
 // Units: one step of a block (32 WT places) for one row tile of one key head.  All units of a call, ordered by sequence, head, row tile
 // and place, are cut into equal runs, one per block, whatever the sequences' lengths; a run may begin and end inside a row tile, whose pieces
-// tree_merge_kernel joins.  The cut depends on the books alone, so results do not change from run to run.
+// tree_merge_rows_kernel or tree_merge_tiles_kernel joins.  The cut depends on the books alone, so results do not change from run to run.
 struct Division { int64_t units; int blocks; };
 __device__ __forceinline__ int64_t run_start(const Division &d, int block)
 {
