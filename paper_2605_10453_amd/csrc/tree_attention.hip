@@ -55,16 +55,19 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
     const float unit = fmaxf(fabsf(call.scale) * kLog2e, 1.2e-38f);    // (not 0: an unseen place's score of -infinity stays one)
     const bool negative = call.scale < 0.f;
 
-    // byte offsets of a lane's loads from the first of 16 places.  Channels past head_dim: the row's first piece again (for K, against
-    // zeros of Q; what V gives there is not stored)
-    uint32_t koff[EXACT ? 1 : kKC], voff[4];
+    // byte offsets of a lane's loads from the first of 16 places.  Channels past head_dim: zeros for K (against zeros of Q; another piece of the
+    // row would make an infinite key's score no number), the row's first piece again for V (what it gives there is not stored)
+    uint32_t voff[4];
     const uint32_t row_bytes = 2 * (uint32_t)c.place_stride;
-#pragma unroll
-    for (int k = 0; k < (EXACT ? 1 : kKC); ++k) koff[k] = r * row_bytes + (32 * k + 8 * g < D ? 2 * (32 * k + 8 * g) : 0);
+    const uint32_t koff = r * row_bytes + 16 * g;
 #pragma unroll
     for (int i = 0; i < 4; ++i) voff[i] = (4 * g + i) * row_bytes + (kVW * r < D ? 2 * kVW * r : 0);
 
     uint4 qf[NQ][kKC], kf[2][kKC];
+    if constexpr (!EXACT) {
+#pragma unroll
+        for (int k = 0; k < kKC; ++k) kf[0][k] = kf[1][k] = make_uint4(0, 0, 0, 0);
+    }
     int page[2], next[2];
     // the query row number x of this lane in a piece: its token and its query head
     auto row_of = [&](const Piece &p, int x, int &t, int &h) {
@@ -108,8 +111,7 @@ __global__ __launch_bounds__(kThreads, DP == 64 && NQ == 1 ? 3 : 2) void tree_ro
             const char *base = reinterpret_cast<const char *>(c.k + offset_of(p, step, a, of[a]));
 #pragma unroll
             for (int k = 0; k < kKC; ++k)
-                if (EXACT) kf[a][k] = *reinterpret_cast<const uint4 *>(base + koff[0] + 64 * k);
-                else if (32 * k < D) kf[a][k] = *reinterpret_cast<const uint4 *>(base + koff[k]);
+                if (EXACT || 32 * k + 8 * g < D) kf[a][k] = *reinterpret_cast<const uint4 *>(base + koff + 64 * k);
         }
     };
 

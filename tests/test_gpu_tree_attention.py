@@ -213,6 +213,31 @@ def test_bad_values_that_a_row_sees_reach_that_row_only(b, T):
     assert torch.equal(got[3][:, keep], want[3][:, keep])
 
 
+@pytest.mark.parametrize("T", [2, 70])
+@pytest.mark.parametrize("D", [8, 40, 64, 72, 80, 120, 128, 136, 256])
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+def test_a_key_of_score_minus_infinity_weighs_nothing(b, D, T, dtype):
+    """A committed key whose infinite channel makes every row's score -infinity: the rows are those of a context without it."""
+    g = torch.Generator().manual_seed(D + T)
+    lens, counts = [75], [T]
+    cache = make_cache(b, g, lens, counts, 1, D, 16, dtype)
+    q = torch.randn(T, 2, D, generator=g)
+    q[:, :, 1] = q[:, :, 1].abs() + 0.5
+    q = q.to(dtype).cuda()
+    page = cache.table.cpu()[0, 2]
+    cache.k[0, page, 0, 5, 1] = -float("inf")
+    slots = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got, lse = b.tree_attention(cache, 0, q, slots, torch.tensor([0, T], dtype=torch.int32, device="cuda"), scale=D ** -0.5)
+    k, v = rows_of(cache, 0, 0, lens[0] + T)
+    seen = torch.arange(lens[0] + T)[None] <= lens[0] + torch.arange(T)[:, None]
+    seen[:, 2 * 16 + 5] = False
+    for h in range(2):
+        ref = attention_reference(q.cpu().double()[:, h], k[:, 0], v[:, 0], seen, D ** -0.5)
+        bound, bound_lse = attention_bounds(*ref, dtype)
+        assert ((got[:, h].cpu().double() - ref[0]).abs() <= bound).all(), h
+        assert ((lse[:, h].cpu().double() - ref[1]).abs() <= bound_lse).all(), h
+
+
 def test_large_scores(b):
     """Scores of thousands, both signs, falling and rising along the context: the running maximum moves at every step, no weight overflows."""
     g = torch.Generator().manual_seed(11)
