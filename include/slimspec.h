@@ -272,8 +272,10 @@ int routed_head_topk_prepared(const void *h, const void *A, const void *B, const
  * slimspec_cache and slimspec_batch themselves are read on the host during the call only.
  * Ownership, asynchrony and errors as above; what stands in device memory cannot be checked before
  * the call returns, so the kernels bound it themselves: a sequence whose slot, token range or
- * length is out of range is left out, a page number out of range counts as no page (nothing is
- * read or written there; attention does not see its tokens).
+ * length is out of range, or whose slot does not hold the pages of its committed and new tokens, is
+ * left out (so a step may go on before the report of a refused slimspec_cache_reserve is read: it
+ * moves and answers nothing of that sequence); a page number out of range counts as no page (nothing
+ * is read or written there; attention does not see its tokens).
  *
  * Supported: BF16 and F16; head_dim a multiple of 8 up to SLIMSPEC_CACHE_MAX_HEAD_DIM; page_size a
  * power of two, 16 to 1024; up to SLIMSPEC_CACHE_MAX_SEQUENCES sequences a call; slot_pages *

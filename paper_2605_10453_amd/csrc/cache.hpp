@@ -20,7 +20,9 @@ struct BatchView { const int32_t *slots, *first; int32_t n, tokens; };
 
 #if defined(__HIPCC__)
 // A sequence of the batch.  What the device arrays say is bounded here once: a sequence out of range has no tokens (tokens = 0, valid = false).
+// HELD: so is one that does not hold the pages of its committed and new tokens (table entries past them are of other times, or other slots).
 struct Sequence { int slot, first, tokens, len; bool valid; };
+template <bool HELD = true>
 __device__ __forceinline__ Sequence sequence_of(const CacheView &c, const BatchView &b, int i)
 {
     Sequence q;
@@ -30,8 +32,9 @@ __device__ __forceinline__ Sequence sequence_of(const CacheView &c, const BatchV
     q.tokens = hi - lo;
     q.valid = q.slot >= 0 && q.slot < c.slots && lo >= 0 && hi >= lo && hi <= b.tokens;
     q.len = q.valid ? c.lens[q.slot] : 0;
-    // places are int32: slot_pages * page_size < 2^31, and lens + tokens must stay inside the table
-    q.valid = q.valid && q.len >= 0 && (int64_t)q.len + q.tokens <= (int64_t)c.slot_pages << c.page_shift;
+    const int pages = HELD && q.valid ? min(c.held[q.slot], c.slot_pages) : c.slot_pages;
+    // places are int32: slot_pages * page_size < 2^31, and lens + tokens must stay inside the pages
+    q.valid = q.valid && q.len >= 0 && (int64_t)q.len + q.tokens <= (int64_t)pages * (1 << c.page_shift);
     if (!q.valid) { q.tokens = 0; q.len = 0; q.first = 0; }
     return q;
 }

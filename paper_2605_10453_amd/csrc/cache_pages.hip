@@ -118,7 +118,7 @@ __global__ __launch_bounds__(kBookThreads) void cache_reserve_kernel(CacheView c
     __shared__ int wave_sums[kBookThreads / 64];
     bool bad = false;
     for (int i = threadIdx.x; i < b.n; i += kBookThreads) {
-        const Sequence q = sequence_of(c, b, i);
+        const Sequence q = sequence_of<false>(c, b, i);
         const int want = (int)(((int64_t)q.len + q.tokens + (1 << c.page_shift) - 1) >> c.page_shift);
         const int held = q.valid ? c.held[q.slot] : 0;
         bad |= !q.valid || held < 0 || held > c.slot_pages;

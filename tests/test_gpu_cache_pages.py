@@ -245,6 +245,37 @@ def test_append_leaves_out_what_has_no_place(b):
     assert cache.k.max().item() == 1 and cache.v.sum().item() == 16 * 2 * 64
 
 
+def test_a_step_goes_on_after_a_refused_reserve(b):
+    """The report is read later: until then the calls leave out the sequences that do not hold their tokens' pages, and nobody's rows are touched."""
+    cache = b.PagedCache.empty(2, 4, 2, 16, 64, 3, 4)
+    rows = lambda n, x: torch.full((2, n, 2, 64), x, dtype=BF, device="cuda")  # noqa: E731
+    assert b.cache_reserve(cache, dev([0, 1]), dev([0, 30, 46])).item() == 0
+    b.cache_append(cache, 0, rows(46, 1.0), rows(46, 2.0), dev([0, 1]), dev([0, 30, 46]))
+    b.cache_set_lens(cache, dev([0, 1]), dev([30, 16]))
+    books = [x.clone() for x in (cache.table, cache.held, cache.lens, cache.refs)]
+    k, v = cache.k.clone(), cache.v.clone()
+    # slot 1 and slot 2 need three pages, one is free; slot 0's two tokens have room
+    slots, first = dev([1, 0, 2]), dev([0, 17, 19, 28])
+    report = b.cache_reserve(cache, slots, first)
+    b.cache_append(cache, 0, rows(28, 5.0), rows(28, 6.0), slots, first)
+    page = books[0][0, 1].item()
+    k[:, page, :, 14:], v[:, page, :, 14:] = 5.0, 6.0
+    assert torch.equal(cache.k, k) and torch.equal(cache.v, v)
+    q = torch.randn(28, 4, 64, device="cuda").to(BF)
+    out, lse = torch.full_like(q, 100.0), torch.full((28, 4), 1e9, device="cuda")
+    b.tree_attention(cache, 0, q, slots, first, out=out, lse=lse)
+    assert (out[:17] == 100).all() and (out[19:] == 100).all() and (lse[:17] == 1e9).all() and (lse[19:] == 1e9).all()
+    assert (out[17:19] != 100).all() and (lse[17:19] != 1e9).all()
+    path = torch.tensor([[1, 2], [1, 0], [0, 1]], dtype=torch.int32, device="cuda")
+    new_lens = b.cache_compact(cache, slots, first, path, dev([2, 1, 2]))
+    assert new_lens.tolist() == [16, 31, 0] and report.item() == 2
+    k[:, page, :, 14], v[:, page, :, 14] = k[:, page, :, 15], v[:, page, :, 15]
+    assert torch.equal(cache.k, k) and torch.equal(cache.v, v)
+    assert all(torch.equal(x, y) for x, y in zip((cache.held, cache.lens, cache.refs), books[1:]))
+    held = torch.arange(cache.table.shape[1], device="cuda")[None] < cache.held[:, None]      # (entries past them mean nothing)
+    assert torch.equal(cache.table[held], books[0][held])
+
+
 @pytest.mark.parametrize("counts", [[1], [8] * 64, [64, 1, 63], [65, 0, 128], [300, 1000], [4096]], ids=str)
 def test_tree_masks(b, counts):
     rng = random.Random(sum(counts))
